@@ -203,6 +203,52 @@ int mdn_recurrent_step(const mdn_shape *shape, const void *q, const void *k, con
                        void *stream);
 
 /*
+ * The gated delta rule, the momentum-free relative of the rule above, with states S in R^{dk x dv} of H value heads; value head h reads the
+ * queries and keys of head h / (H / Hk):
+ *     e_t = v_t - e^{g_t} S_{t-1}^T k_t        S_t = e^{g_t} S_{t-1} + beta_t k_t e_t^T        o_t = scale * S_t^T q_t
+ * Token tensors are contiguous: q, k [B,T,Hk,dk], v, o, e [B,T,H,dv] in the storage dtype; g, beta [B,T,H] fp32; states [sequences,H,dk,dv]
+ * fp32.  dk and dv each in {64, 128}, H a multiple of Hk and at most 4096, any T >= 1, chunks of 64 tokens (the last one of a sequence
+ * may be partial).  g is the LOGARITHM of the decay, so that it has a gradient however strong the decay is: meant to be <= 0; 0 keeps the
+ * state, -inf (and whatever is below log 2^-200, of whatever the gradient is then 0 in fp32) drops it.
+ * Packed batches: cu_seqlens is a HOST array of n_seq + 1 increasing offsets from 0 to T (read before the call returns) and B = 1; sequences
+ * of equal lengths: cu_seqlens NULL, n_seq 0.  A NaN or infinity in a token reaches the outputs of its 64-token chunk and what follows it.
+ * With 16-bit storage the products take bf16 operands and sum in fp32.  A state that leaves the call in 32 bits (S_final, dS0) is carried with
+ * operands of twice the bits (value + remainder) and is good to about 2^-17; ask for it only where it is wanted.  States the backward keeps
+ * for itself are rounded to the storage dtype.  All pointers 16-byte aligned.  Results do not depend on anything but the arguments:
+ * repeated calls agree bit for bit.  No call synchronises or allocates; launches are not recorded by the timing facility below.
+ */
+typedef struct mdn_gdr_shape {
+    int32_t B, T, H, Hk; /* batch, sequence length, value heads, key heads */
+    int32_t dk, dv;
+    int32_t dtype;       /* MDN_DTYPE_* */
+    float scale;         /* multiplies q; usually dk^-1/2 */
+} mdn_gdr_shape;
+
+enum { MDN_GDR_WS_FWD = 0, MDN_GDR_WS_BWD = 1, MDN_GDR_STATES = 2, MDN_GDR_OPERANDS = 3 };
+/* Bytes of the workspace of the forward / backward call and of the optional buffers states_saved and operands_saved.  Host-only. */
+int mdn_gdr_bytes(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int32_t n_seq, int which, size_t *bytes_out);
+
+/* Forward.  S0 may be NULL (= 0); S_final, e_saved [B,T,H,dv] (the corrections e, which the backward needs), states_saved (the chunk-start
+ * states) and operands_saved (chunk-local operands of the reverse pass) may be NULL (not written).  S_final may be the memory of S0. */
+int mdn_gdr_chunk_fwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int32_t n_seq, const void *q, const void *k, const void *v,
+                      const float *g, const float *beta, const float *S0, void *o, float *S_final, void *e_saved, void *states_saved,
+                      void *operands_saved, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Backward, for L = <o, dO> + <S_final, dS_final>, from the forward's inputs (v is not needed) and e_saved.  Without states_saved /
+ * operands_saved (NULL) the backward forms them again; with dS0 asked for and 16-bit storage it forms the operands again in any case.
+ * dS_final may be NULL (= 0), dS0 may be NULL (not wanted) or the memory of S0 or of dS_final.
+ * dq, dk [B,T,Hk,dk] are summed over the value heads of a key head (in 32 bits), dv [B,T,H,dv]; dg, dbeta [B,T,H] are in the STORAGE dtype: what
+ * products of 16-bit operands say about a gate is good to as many bits. */
+int mdn_gdr_chunk_bwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int32_t n_seq, const void *q, const void *k, const float *g,
+                      const float *beta, const float *S0, const void *e_saved, const void *states_saved, const void *operands_saved,
+                      const void *dO, const float *dS_final, void *dq, void *dk, void *dv, void *dg, void *dbeta, float *dS0,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/* Token by token (decoding): S [B,H,dk,dv] is advanced in place over the T tokens given; fp32 arithmetic throughout. */
+int mdn_gdr_recurrent_step(const mdn_gdr_shape *shape, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                           float *S, void *o, void *stream);
+
+/*
  * Stability-aware gate parameterisation (Sec. 3.3, "Stability Aware Gating Parameterization"): from the four
  * per-head projections of every token to the linear-domain gates that mdn_chunk_fwd / mdn_recurrent_step take,
  *     eta   = tanh(x_eta / tau) + 1,    theta = arctan(eta s),   alpha_max = cos^2 theta,   beta_max = sin^2 theta,

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libmdn_hip.so")
 
 MDN_DTYPE_BF16, MDN_DTYPE_F32 = 0, 1
 MDN_WS_FWD, MDN_WS_BWD, MDN_WS_BWD_STATE_ADJOINTS = 0, 1, 2
+MDN_GDR_WS_FWD, MDN_GDR_WS_BWD, MDN_GDR_STATES, MDN_GDR_OPERANDS = 0, 1, 2, 3
 MDN_WS_FWD_NO_STATES, MDN_WS_BWD_NO_STATES, MDN_WS_BWD_NO_STATE_ADJOINTS = 3, 4, 5 # packed batches only
 
 EXPORTS = ("mdn_version", "mdn_strerror", "mdn_workspace_bytes", "mdn_saved_states_bytes",
@@ -27,7 +28,8 @@ EXPORTS = ("mdn_version", "mdn_strerror", "mdn_workspace_bytes", "mdn_saved_stat
            "mdn_chunk_bwd", "mdn_recurrent_step", "mdn_profile_begin", "mdn_profile_end", "mdn_profile_begin_sampled",
            "mdn_profile_launch_counts", "mdn_set_segments",
            "mdn_gates_fwd", "mdn_gates_bwd", "mdn_frontend_fwd", "mdn_frontend_bwd", "mdn_epilogue_fwd",
-           "mdn_epilogue_bwd", "mdn_workspace_bytes_varlen", "mdn_chunk_fwd_varlen", "mdn_chunk_bwd_varlen")
+           "mdn_epilogue_bwd", "mdn_workspace_bytes_varlen", "mdn_chunk_fwd_varlen", "mdn_chunk_bwd_varlen",
+           "mdn_gdr_bytes", "mdn_gdr_chunk_fwd", "mdn_gdr_chunk_bwd", "mdn_gdr_recurrent_step")
 
 KERNEL_NAMES = ("intra_fwd", "scan_fwd", "intra_bwd", "rebuild", "scan_bwd", "grad", "recurrent")
 
@@ -41,6 +43,11 @@ class MdnGateParams(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("a_alpha", ctypes.c_void_p),
                 ("b_alpha", ctypes.c_void_p), ("a_mu", ctypes.c_void_p), ("b_mu", ctypes.c_void_p),
                 ("s", ctypes.c_float), ("tau", ctypes.c_float), ("mu_log_min", ctypes.c_float)]
+
+
+class MdnGdrShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("dk", ctypes.c_int32),
+                ("dv", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class MdnError(RuntimeError):
@@ -108,6 +115,15 @@ def load_library():
     lib.mdn_epilogue_fwd.argtypes = [sp, vp, vp, fp, cf, vp, vp]
     lib.mdn_epilogue_bwd.restype = ctypes.c_int
     lib.mdn_epilogue_bwd.argtypes = [sp, vp, vp, fp, cf, vp, vp, vp, fp, vp]
+    gs = ctypes.POINTER(MdnGdrShape)
+    lib.mdn_gdr_bytes.restype = ctypes.c_int
+    lib.mdn_gdr_bytes.argtypes = [gs, ip, ctypes.c_int32, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
+    lib.mdn_gdr_chunk_fwd.restype = ctypes.c_int
+    lib.mdn_gdr_chunk_fwd.argtypes = [gs, ip, ctypes.c_int32] + [vp] * 12 + [ctypes.c_size_t, vp]
+    lib.mdn_gdr_chunk_bwd.restype = ctypes.c_int
+    lib.mdn_gdr_chunk_bwd.argtypes = [gs, ip, ctypes.c_int32] + [vp] * 17 + [ctypes.c_size_t, vp]
+    lib.mdn_gdr_recurrent_step.restype = ctypes.c_int
+    lib.mdn_gdr_recurrent_step.argtypes = [gs] + [vp] * 8
     _lib = lib
     return lib
 
@@ -264,3 +280,36 @@ def mdn_chunk_bwd_varlen(q, k, v, beta, alpha, mu, vt, dO, cu_seqlens, eta=None,
     None with want_state_grads=False."""
     return (_host or _load_host()).chunk_bwd_varlen(q, k, v, beta, alpha, mu, vt, dO, cu_seqlens, eta, S0, M0, dS_final, dM_final,
                                                     scale, want_deta, want_state_grads)
+
+
+def gdr_bytes(shape: MdnGdrShape, which: int, cu_seqlens=None) -> int:
+    """Bytes of the workspace of mdn_gdr_chunk_fwd / mdn_gdr_chunk_bwd or of one of the optional buffers (MDN_GDR_*)."""
+    n = ctypes.c_size_t(0)
+    cu = None if cu_seqlens is None else (ctypes.c_int32 * len(cu_seqlens))(*cu_seqlens)
+    _check(load_library().mdn_gdr_bytes(ctypes.byref(shape), cu, 0 if cu is None else len(cu_seqlens) - 1, which, ctypes.byref(n)),
+           "mdn_gdr_bytes")
+    return n.value
+
+
+def mdn_gdr_chunk_fwd(q, k, v, g, beta, S0=None, scale=None, cu_seqlens=None, save_e=False, save_states=False, save_operands=False,
+                      output_final_state=True, workspace=None, out=None):
+    """Gated delta rule, chunkwise: q, k [B, T, Hk, dk], v [B, T, H, dv] (H a multiple of Hk), log decays g and step sizes beta [B, T, H] fp32,
+    S0 [B, H, dk, dv] fp32; packed sequences: B = 1 and cu_seqlens, a host sequence of n + 1 offsets, states [n, H, dk, dv].  Returns a
+    dict: o, S (final states or None; with 16-bit storage they cost a slower call), e, states, operands (or None; what the backward can
+    use), workspace; `out`: such a dict, whose tensors are reused."""
+    return (_host or _load_host()).gdr_chunk_fwd(q, k, v, g, beta, S0, scale, cu_seqlens, save_e, save_states, save_operands,
+                                                 output_final_state, workspace, out)
+
+
+def mdn_gdr_chunk_bwd(q, k, g, beta, e, dO, S0=None, states=None, operands=None, dS_final=None, scale=None, cu_seqlens=None,
+                      want_dS0=False, workspace=None, out=None):
+    """Adjoint of mdn_gdr_chunk_fwd from its inputs and its e (states, operands: the forward's, or formed again).  Returns a dict: dq, dk
+    (summed over the value heads of a key head), dv, dg, dbeta (all in q's dtype), dS0 (fp32 or None), workspace; `out`: such a dict, whose
+    tensors are reused."""
+    return (_host or _load_host()).gdr_chunk_bwd(q, k, g, beta, e, dO, S0, states, operands, dS_final, scale, cu_seqlens, want_dS0,
+                                                 workspace, out)
+
+
+def mdn_gdr_recurrent_step(q, k, v, g, beta, S, scale=None, out=None):
+    """Gated delta rule over the T tokens given, one after the other; S [B, H, dk, dv] fp32 is updated in place.  Returns o."""
+    return (_host or _load_host()).gdr_recurrent_step(q, k, v, g, beta, S, scale, out)

@@ -1,0 +1,262 @@
+// C ABI of the gated delta rule: argument checks, workspace carving, kernel sequencing.  The contract is in include/mdn.h.
+#include "../../include/mdn.h"
+#include "mdn_gdr.h"
+
+#include <hip/hip_runtime.h>
+#include <algorithm>
+#include <new>
+#include <vector>
+
+using namespace mdn;
+
+namespace {
+
+struct Carve {
+    char *base;
+    size_t off = 0;
+    explicit Carve(void *b) : base(static_cast<char *>(b)) {}
+    template <typename P = void> P *take(size_t bytes) {
+        char *p = base ? base + off : nullptr;
+        off += (bytes + 255) / 256 * 256;
+        return reinterpret_cast<P *>(p);
+    }
+};
+
+int check_shape(const mdn_gdr_shape *s, GdrDims *d) {
+    if (!s) return MDN_ERR_NULL;
+    if (s->dtype != MDN_DTYPE_BF16 && s->dtype != MDN_DTYPE_F32) return MDN_ERR_DTYPE;
+    if (s->B < 1 || s->T < 1 || s->H < 1 || s->Hk < 1 || s->H > 4096 || s->H % s->Hk) return MDN_ERR_SHAPE;
+    if ((s->dk != 64 && s->dk != 128) || (s->dv != 64 && s->dv != 128)) return MDN_ERR_SHAPE;
+    if ((long long)s->B * s->H > (1 << 24) || ((long long)s->B * s->T + 64) * s->H > (1LL << 31) - 1) return MDN_ERR_SHAPE;
+    *d = GdrDims{};
+    d->B = s->B; d->T = s->T; d->H = s->H; d->Hk = s->Hk;
+    d->N = (int)(((long long)s->T + 63) / 64);
+    d->nchunks = (int)((long long)s->B * d->N);
+    d->dk = s->dk; d->dv = s->dv; d->dtype = s->dtype; d->scale = s->scale;
+    return MDN_OK;
+}
+
+// cu: null for sequences of equal lengths
+int check(const mdn_gdr_shape *s, const int32_t *cu, int32_t n_seq, GdrDims *d) {
+    const int rc = check_shape(s, d);
+    if (rc) return rc;
+    if (!cu) return n_seq ? MDN_ERR_NULL : MDN_OK;
+    if (s->B != 1 || n_seq < 1 || (long long)n_seq * s->H > (1 << 24)) return MDN_ERR_SHAPE;
+    if (cu[0] != 0 || cu[n_seq] != s->T) return MDN_ERR_SHAPE;
+    long long chunks = 0, longest = 0;
+    for (int i = 0; i < n_seq; ++i) {
+        if (cu[i + 1] <= cu[i] || cu[i + 1] > s->T) return MDN_ERR_SHAPE;
+        const long long n = ((long long)cu[i + 1] - cu[i] + 63) / 64;
+        chunks += n;
+        longest = std::max(longest, n);
+    }
+    d->B = n_seq;
+    d->N = (int)longest;
+    d->nchunks = (int)chunks;
+    return MDN_OK;
+}
+
+size_t elem(const GdrDims &d) { return d.dtype == MDN_DTYPE_F32 ? 4 : 2; }
+size_t blocks(const GdrDims &d) { return (size_t)d.nchunks * d.H; }
+size_t states_bytes(const GdrDims &d) { return blocks(d) * d.dk * d.dv * elem(d); }
+
+struct Tables { SeqEntry *seqs; ChunkEntry *chunks; };
+Tables carve_tables(Carve &c, const GdrDims &d, bool packed) {
+    Tables t = {};
+    if (packed) {
+        t.seqs = c.take<SeqEntry>((size_t)d.B * sizeof(SeqEntry));
+        t.chunks = c.take<ChunkEntry>((size_t)d.nchunks * sizeof(ChunkEntry));
+    }
+    return t;
+}
+// from the host's offsets, which travel in kernel arguments
+int build_tables(GdrDims *d, const Tables &t, const int32_t *cu, hipStream_t s) {
+    if (!cu) return MDN_OK;
+    std::vector<SeqEntry> e;
+    try {
+        e.resize(d->B);
+    } catch (const std::bad_alloc &) {
+        return MDN_ERR_LAUNCH;
+    }
+    int cb = 0;
+    for (int i = 0; i < d->B; ++i) {
+        e[i] = SeqEntry{cu[i], cu[i + 1] - cu[i], cb, i};
+        cb += (int)(((long long)e[i].len + 63) / 64);
+    }
+    // the longest first: their scans are what the others run beside
+    std::sort(e.begin(), e.end(), [](const SeqEntry &a, const SeqEntry &b) { return a.len != b.len ? a.len > b.len : a.t0 < b.t0; });
+    SeqList l;
+    l.H = d->H;
+    for (l.first = 0; l.first < d->B; l.first += l.n) {
+        l.n = std::min(d->B - l.first, kSeqsPerLaunch);
+        std::copy(e.begin() + l.first, e.begin() + l.first + l.n, l.e);
+        if (launch_seq_tables(l, t.seqs, t.chunks, s) != hipSuccess) return MDN_ERR_LAUNCH;
+    }
+    d->seqs = t.seqs;
+    d->chunks = t.chunks;
+    return MDN_OK;
+}
+
+struct FwdWs { Tables tables; float *coef; void *T, *T_lo, *P; size_t total; };
+FwdWs carve_fwd(const GdrDims &d, bool packed, void *ws) {
+    Carve c(ws);
+    FwdWs w;
+    const size_t tri = blocks(d) * gdr_triangle_bytes(d.dtype);
+    w.tables = carve_tables(c, d, packed);
+    w.coef = c.take<float>(blocks(d) * kGdrCoef * sizeof(float));
+    w.T = c.take(tri);
+    w.T_lo = d.dtype == MDN_DTYPE_BF16 ? c.take(tri) : nullptr;
+    w.P = c.take(tri);
+    w.total = c.off;
+    return w;
+}
+
+struct Operands { float *coef; void *TT, *PT; size_t total; };
+Operands carve_operands(const GdrDims &d, void *p) {
+    Carve c(p);
+    Operands w;
+    const size_t tri = blocks(d) * gdr_triangle_bytes(d.dtype);
+    w.coef = c.take<float>(blocks(d) * kGdrCoef * sizeof(float));
+    w.TT = c.take(tri);
+    w.PT = c.take(tri);
+    w.total = c.off;
+    return w;
+}
+
+struct BwdWs { Tables tables; Operands op; void *TT_lo, *PT_lo, *states, *dstates, *sums; size_t total; };
+BwdWs carve_bwd(const GdrDims &d, bool packed, void *ws) {
+    Carve c(ws);
+    BwdWs w;
+    const size_t tri = blocks(d) * gdr_triangle_bytes(d.dtype);
+    w.tables = carve_tables(c, d, packed);
+    void *op = c.take(carve_operands(d, nullptr).total);
+    w.op = carve_operands(d, op);
+    w.TT_lo = d.dtype == MDN_DTYPE_BF16 ? c.take(tri) : nullptr;
+    w.PT_lo = d.dtype == MDN_DTYPE_BF16 ? c.take(tri) : nullptr;
+    w.states = c.take(states_bytes(d));
+    w.dstates = c.take(states_bytes(d));
+    w.sums = d.H > d.Hk ? c.take((size_t)d.nchunks * d.Hk * gdr_sums_bytes(d.dk)) : nullptr;
+    w.total = c.off;
+    return w;
+}
+
+int status(hipError_t e) { return e == hipSuccess ? MDN_OK : MDN_ERR_LAUNCH; }
+
+template <size_t N> int check_pointers(const void *const (&required)[N], std::initializer_list<const void *> optional) {
+    for (const void *p : required)
+        if (!p) return MDN_ERR_NULL;
+    for (const void *p : required)
+        if (reinterpret_cast<uintptr_t>(p) & 15u) return MDN_ERR_ALIGN;
+    for (const void *p : optional)
+        if (reinterpret_cast<uintptr_t>(p) & 15u) return MDN_ERR_ALIGN;
+    return MDN_OK;
+}
+
+} // namespace
+
+extern "C" {
+
+int mdn_gdr_bytes(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int32_t n_seq, int which, size_t *bytes_out) {
+    if (!bytes_out) return MDN_ERR_NULL;
+    GdrDims d;
+    const int rc = check(shape, cu_seqlens, n_seq, &d);
+    if (rc) return rc;
+    switch (which) {
+    case MDN_GDR_WS_FWD: *bytes_out = carve_fwd(d, cu_seqlens != nullptr, nullptr).total; return MDN_OK;
+    case MDN_GDR_WS_BWD: *bytes_out = carve_bwd(d, cu_seqlens != nullptr, nullptr).total; return MDN_OK;
+    case MDN_GDR_STATES: *bytes_out = states_bytes(d); return MDN_OK;
+    case MDN_GDR_OPERANDS: *bytes_out = carve_operands(d, nullptr).total; return MDN_OK;
+    default: return MDN_ERR_SHAPE;
+    }
+}
+
+int mdn_gdr_chunk_fwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int32_t n_seq, const void *q, const void *k, const void *v,
+                      const float *g, const float *beta, const float *S0, void *o, float *S_final, void *e_saved, void *states_saved,
+                      void *operands_saved, void *workspace, size_t workspace_bytes, void *stream) {
+    GdrDims d;
+    int rc = check(shape, cu_seqlens, n_seq, &d);
+    if (rc) return rc;
+    const void *const required[] = {q, k, v, g, beta, o, workspace};
+    rc = check_pointers(required, {S0, S_final, e_saved, states_saved, operands_saved});
+    if (rc) return rc;
+    const FwdWs w = carve_fwd(d, cu_seqlens != nullptr, workspace);
+    if (workspace_bytes < w.total) return MDN_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = build_tables(&d, w.tables, cu_seqlens, s);
+    if (rc) return rc;
+    const bool precise = d.dtype == MDN_DTYPE_BF16 && S_final;
+    GdrLocalArgs l = {};
+    l.q = q; l.k = k; l.g = g; l.beta = beta;
+    l.coef = w.coef; l.T = w.T; l.T_lo = precise ? w.T_lo : nullptr; l.P = w.P;
+    if (operands_saved) {
+        const Operands op = carve_operands(d, operands_saved);
+        l.coef = op.coef; l.TT = op.TT; l.PT = op.PT;
+    }
+    rc = status(launch_gdr_local(d, l, s));
+    if (rc) return rc;
+    GdrScanFwdArgs a = {};
+    a.q = q; a.k = k; a.v = v; a.coef = l.coef; a.T = l.T; a.T_lo = l.T_lo; a.P = l.P; a.S0 = S0;
+    a.o = o; a.e = e_saved; a.states = states_saved; a.S_final = S_final;
+    return status(launch_gdr_scan_fwd(d, a, precise, s));
+}
+
+int mdn_gdr_chunk_bwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int32_t n_seq, const void *q, const void *k, const float *g,
+                      const float *beta, const float *S0, const void *e_saved, const void *states_saved, const void *operands_saved,
+                      const void *dO, const float *dS_final, void *dq, void *dk, void *dv, void *dg, void *dbeta, float *dS0,
+                      void *workspace, size_t workspace_bytes, void *stream) {
+    GdrDims d;
+    int rc = check(shape, cu_seqlens, n_seq, &d);
+    if (rc) return rc;
+    const void *const required[] = {q, k, g, beta, e_saved, dO, dq, dk, dv, dg, dbeta, workspace};
+    rc = check_pointers(required, {S0, states_saved, operands_saved, dS_final, dS0});
+    if (rc) return rc;
+    const BwdWs w = carve_bwd(d, cu_seqlens != nullptr, workspace);
+    if (workspace_bytes < w.total) return MDN_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = build_tables(&d, w.tables, cu_seqlens, s);
+    if (rc) return rc;
+    const bool precise = d.dtype == MDN_DTYPE_BF16 && dS0;
+    Operands op = w.op;
+    if (operands_saved && !precise) { // (the forward's have no remainders)
+        op = carve_operands(d, const_cast<void *>(operands_saved));
+    } else {
+        GdrLocalArgs l = {};
+        l.q = q; l.k = k; l.g = g; l.beta = beta;
+        l.coef = op.coef; l.TT = op.TT; l.PT = op.PT;
+        if (precise) l.TT_lo = w.TT_lo, l.PT_lo = w.PT_lo;
+        rc = status(launch_gdr_local(d, l, s));
+        if (rc) return rc;
+    }
+    const void *states = states_saved;
+    if (!states) { // before anything is written over S0
+        GdrScanFwdArgs a = {};
+        a.k = k; a.v = e_saved; a.coef = op.coef; a.S0 = S0; a.states = w.states;
+        rc = status(launch_gdr_rebuild(d, a, s));
+        if (rc) return rc;
+        states = w.states;
+    }
+    GdrScanBwdArgs b = {};
+    b.q = q; b.k = k; b.dO = dO; b.coef = op.coef; b.TT = op.TT; b.PT = op.PT;
+    if (precise) b.TT_lo = w.TT_lo, b.PT_lo = w.PT_lo;
+    b.dS_final = dS_final; b.dv = dv; b.dstates = w.dstates; b.dS0 = dS0;
+    rc = status(launch_gdr_scan_bwd(d, b, precise, s));
+    if (rc) return rc;
+    GdrGradArgs c = {};
+    c.q = q; c.k = k; c.e = e_saved; c.dO = dO; c.dv = dv; c.g = g; c.beta = beta; c.states = states; c.dstates = w.dstates;
+    c.sums = w.sums; c.dq = dq; c.dk = dk; c.dg = dg; c.dbeta = dbeta;
+    return status(launch_gdr_grad(d, c, s));
+}
+
+int mdn_gdr_recurrent_step(const mdn_gdr_shape *shape, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                           float *S, void *o, void *stream) {
+    GdrDims d;
+    int rc = check_shape(shape, &d);
+    if (rc) return rc;
+    const void *const required[] = {q, k, v, g, beta, S, o};
+    rc = check_pointers(required, {});
+    if (rc) return rc;
+    GdrStepArgs a = {q, k, v, g, beta, S, o};
+    return status(launch_gdr_step(d, a, static_cast<hipStream_t>(stream)));
+}
+
+} // extern "C"

@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -459,6 +460,129 @@ PyObject *chunk_bwd_varlen(PyObject *const *x) {
     return r.release();
 }
 
+// ---- the gated delta rule
+
+// the tensors' device as the current one while the call runs, and its stream
+struct OnDevice {
+    c10::DeviceGuard guard;
+    void *stream;
+    explicit OnDevice(const at::Tensor &t) : guard((on_gpu(t), t.device())), stream((void *)c10::hip::getCurrentHIPStream(t.device().index()).stream()) {}
+};
+
+// q k [v] g beta, S0 and cu_seqlens, checked against q (and v, or e in its place)
+struct GdrInputs {
+    const at::Tensor &q, &k, &v, &g, &beta;
+    Opt S0;
+    std::vector<int32_t> cu;
+    mdn_gdr_shape s;
+    at::ScalarType dt;
+    int64_t B, T, H, Hk, dk, dv, seqs;
+    GdrInputs(PyObject *q_, PyObject *k_, PyObject *v_, const char *v_name, PyObject *g_, PyObject *beta_, PyObject *S0_, PyObject *scale, PyObject *cu_)
+        : q(need(q_, "q")), k(need(k_, "k")), v(need(v_, v_name)), g(need(g_, "g")), beta(need(beta_, "beta")), S0(opt(S0_, "S0")) {
+        if (q.dim() != 4 || v.dim() != 4) fail(std::string("q, ") + v_name + " must be [B, T, heads, d]; got " + str(q.sizes()) + ", " + str(v.sizes()));
+        s.dtype = dtype_code(q);
+        dt = q.scalar_type();
+        B = q.size(0); T = q.size(1); Hk = q.size(2); dk = q.size(3); H = v.size(2); dv = v.size(3);
+        if (Hk < 1 || H < 1 || H % Hk) fail("the heads of " + std::string(v_name) + " (" + std::to_string(H) + ") must be a multiple of those of q (" + std::to_string(Hk) + ")");
+        for (int64_t n : {B, T, H})
+            if (n > 0x7fffffff) fail("sizes must fit 32 bits");
+        expect("k", &k, {B, T, Hk, dk}, dt, q);
+        expect(v_name, &v, {B, T, H, dv}, dt, q);
+        expect("g", &g, {B, T, H}, at::kFloat, q);
+        expect("beta", &beta, {B, T, H}, at::kFloat, q);
+        if (!q.is_contiguous()) fail("q must be contiguous");
+        if (cu_ && cu_ != Py_None) {
+            if (B != 1) fail("packed batches are [1, T, heads, d]; got q " + str(q.sizes()));
+            cu = offsets(cu_, T);
+        }
+        seqs = cu.empty() ? B : (int64_t)cu.size() - 1;
+        expect("S0", S0, {seqs, H, dk, dv}, at::kFloat, q);
+        s.B = (int32_t)B; s.T = (int32_t)T; s.H = (int32_t)H; s.Hk = (int32_t)Hk; s.dk = (int32_t)dk; s.dv = (int32_t)dv;
+        s.scale = (float)(scale && scale != Py_None ? number(scale) : std::pow((double)dk, -0.5));
+    }
+    const int32_t *offs() const { return cu.empty() ? nullptr : cu.data(); }
+    int32_t n_offs() const { return cu.empty() ? 0 : (int32_t)cu.size() - 1; }
+    size_t bytes(int which) const {
+        size_t n = 0;
+        check(mdn_gdr_bytes(&s, offs(), n_offs(), which, &n), "mdn_gdr_bytes");
+        return n;
+    }
+};
+
+// q k v g beta | S0 scale cu_seqlens save_e save_states save_operands output_final_state workspace out
+PyObject *gdr_chunk_fwd(PyObject *const *x) {
+    const GdrInputs in(x[0], x[1], x[2], "v", x[3], x[4], x[5], x[6], x[7]);
+    PyObject *out = x[13];
+    const size_t need_ws = in.bytes(MDN_GDR_WS_FWD);
+    at::Tensor o = output(out, "o", {in.B, in.T, in.H, in.dv}, in.dt, in.q);
+    c10::optional<at::Tensor> S, e, states, operands;
+    if (truth(x[11])) S = output(out, "S", {in.seqs, in.H, in.dk, in.dv}, at::kFloat, in.q);
+    if (truth(x[8])) e = output(out, "e", {in.B, in.T, in.H, in.dv}, in.dt, in.q);
+    if (truth(x[9])) states = output_bytes(out, "states", in.bytes(MDN_GDR_STATES), in.q);
+    if (truth(x[10])) operands = output_bytes(out, "operands", in.bytes(MDN_GDR_OPERANDS), in.q);
+    at::Tensor ws = workspace(x[12], need_ws, in.q);
+    const OnDevice dev(in.q);
+    call("mdn_gdr_chunk_fwd", mdn_gdr_chunk_fwd, &in.s, in.offs(), in.n_offs(), ptr(in.q), ptr(in.k), ptr(in.v), ptr<float>(in.g),
+         ptr<float>(in.beta), ptr<float>(in.S0), ptr(o), ptr<float>(S), ptr(e), ptr(states), ptr(operands), ptr(ws), size_of(ws), dev.stream);
+    Dict r;
+    r.set("o", o);
+    r.set("S", S);
+    r.set("e", e);
+    r.set("states", states);
+    r.set("operands", operands);
+    r.set("workspace", ws);
+    return r.release();
+}
+
+// q k g beta e dO | S0 states operands dS_final scale cu_seqlens want_dS0 workspace out
+PyObject *gdr_chunk_bwd(PyObject *const *x) {
+    const GdrInputs in(x[0], x[1], x[4], "e", x[2], x[3], x[6], x[10], x[11]);
+    const at::Tensor &dO = need(x[5], "dO");
+    Opt states = opt(x[7], "states"), operands = opt(x[8], "operands"), dS = opt(x[9], "dS_final");
+    const size_t need_ws = in.bytes(MDN_GDR_WS_BWD);
+    expect("dO", &dO, {in.B, in.T, in.H, in.dv}, in.dt, in.q);
+    expect("dS_final", dS, {in.seqs, in.H, in.dk, in.dv}, at::kFloat, in.q);
+    if (states) expect_bytes("states", states, in.bytes(MDN_GDR_STATES), in.q);
+    if (operands) expect_bytes("operands", operands, in.bytes(MDN_GDR_OPERANDS), in.q);
+    PyObject *out = x[14];
+    at::Tensor dq = output(out, "dq", {in.B, in.T, in.Hk, in.dk}, in.dt, in.q), dk = output(out, "dk", {in.B, in.T, in.Hk, in.dk}, in.dt, in.q),
+               dv = output(out, "dv", {in.B, in.T, in.H, in.dv}, in.dt, in.q), dg = output(out, "dg", {in.B, in.T, in.H}, in.dt, in.q),
+               db = output(out, "dbeta", {in.B, in.T, in.H}, in.dt, in.q);
+    c10::optional<at::Tensor> dS0;
+    if (truth(x[12])) dS0 = output(out, "dS0", {in.seqs, in.H, in.dk, in.dv}, at::kFloat, in.q);
+    at::Tensor ws = workspace(x[13], need_ws, in.q);
+    const OnDevice dev(in.q);
+    call("mdn_gdr_chunk_bwd", mdn_gdr_chunk_bwd, &in.s, in.offs(), in.n_offs(), ptr(in.q), ptr(in.k), ptr<float>(in.g), ptr<float>(in.beta),
+         ptr<float>(in.S0), ptr(in.v), ptr(states), ptr(operands), ptr(dO), ptr<float>(dS), ptr(dq), ptr(dk), ptr(dv), ptr(dg), ptr(db),
+         ptr<float>(dS0), ptr(ws), size_of(ws), dev.stream);
+    Dict r;
+    r.set("dq", dq);
+    r.set("dk", dk);
+    r.set("dv", dv);
+    r.set("dg", dg);
+    r.set("dbeta", db);
+    r.set("dS0", dS0);
+    r.set("workspace", ws);
+    return r.release();
+}
+
+// q k v g beta S | scale out
+PyObject *gdr_recurrent_step(PyObject *const *x) {
+    const GdrInputs in(x[0], x[1], x[2], "v", x[3], x[4], x[5], x[6], nullptr);
+    if (!in.S0) fail("S is required (it is advanced in place)");
+    Opt given = opt(x[7], "out");
+    expect("out", given, {in.B, in.T, in.H, in.dv}, in.dt, in.q);
+    at::Tensor o = given ? *given : empty({in.B, in.T, in.H, in.dv}, in.dt, in.q);
+    const OnDevice dev(in.q);
+    call("mdn_gdr_recurrent_step", mdn_gdr_recurrent_step, &in.s, ptr(in.q), ptr(in.k), ptr(in.v), ptr<float>(in.g), ptr<float>(in.beta),
+         ptr<float>(in.S0), ptr(o), dev.stream);
+    if (given) {
+        Py_INCREF(x[7]);
+        return x[7];
+    }
+    return THPVariable_Wrap(o);
+}
+
 // the four projections x_alpha x_mu x_beta x_eta, the four per-head vectors, and the scalars
 struct GateInputs {
     const at::Tensor &xa, &xm, &xb, &xe;
@@ -671,6 +795,7 @@ PyMethodDef methods[] = {MDN_ENTRY(chunk_fwd, 17), MDN_ENTRY(chunk_fwd_noalloc, 
                          MDN_ENTRY(recurrent_step, 11), MDN_ENTRY(chunk_fwd_varlen, 13), MDN_ENTRY(chunk_bwd_varlen, 17),
                          MDN_ENTRY(gates_fwd, 11), MDN_ENTRY(gates_bwd, 16), MDN_ENTRY(frontend_fwd, 5),
                          MDN_ENTRY(frontend_bwd, 9), MDN_ENTRY(epilogue_fwd, 4), MDN_ENTRY(epilogue_bwd, 6),
+                         MDN_ENTRY(gdr_chunk_fwd, 14), MDN_ENTRY(gdr_chunk_bwd, 15), MDN_ENTRY(gdr_recurrent_step, 8),
                          {"set_error_types", set_error_types, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mdn_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
