@@ -297,6 +297,39 @@ int mdn_epilogue_bwd(const mdn_shape *shape, const void *o, const void *g, const
                      void *d_o, void *dg, float *dw, void *stream);
 
 /*
+ * 8-bit checkpoints of what the backward of the front end and the back end needs again: x_q, x_k, x_v and o, g, which a training step
+ * otherwise keeps in the storage dtype from the forward to the backward.  A tensor [B,T,H,d] is kept as int8 codes [B,T,H,d] and exponent bytes
+ * [B,T,H,d/32]: of every 32 values the step 2^(e - 127) = 2^(floor(log2 max) - 6) (at least 2^-126) and code = round-to-even(x / step), at
+ * most 127 in size; x reads back as code * step, exactly, off by at most half a step (a whole one where the code was limited).  A block that
+ * holds an infinity or a NaN reads back as NaN.  shape and eps as above (dk = dv).
+ *   mdn_keep / mdn_kept_values            a tensor [B,T,H,d] in the storage dtype to its checkpoint, and back
+ *   mdn_frontend_fwd_keep                 mdn_frontend_fwd that also writes the checkpoints of x_q, x_k, x_v (kept[3]): same q, k, v
+ *   mdn_frontend_fwd_kept                 q, k, v from the checkpoints: what the rule's backward reads, which need not be kept then
+ *   mdn_frontend_bwd_kept                 mdn_frontend_bwd at the values that the checkpoints read back as
+ *   mdn_epilogue_fwd_keep, mdn_epilogue_bwd_kept   the same for the back end: o, g (kept[2])
+ * kept is a HOST array.  Parameter gradients (dd [H], dw [dv]; NULL = not wanted, then workspace may be NULL) are summed in a fixed order:
+ * repeated calls agree bit for bit.  workspace: mdn_kept_workspace_bytes, 4-byte aligned.  Tensors and codes need no alignment but their elements'.
+ * Errors: MDN_ERR_NULL, MDN_ERR_SHAPE, MDN_ERR_DTYPE, MDN_ERR_ALIGN, MDN_ERR_WORKSPACE, MDN_ERR_LAUNCH.
+ */
+typedef struct mdn_kept {
+    int8_t *codes;      /* device, [B,T,H,d] */
+    uint8_t *exponents; /* device, [B,T,H,d/32] */
+} mdn_kept;
+
+int mdn_kept_workspace_bytes(const mdn_shape *shape, size_t *bytes_out);
+int mdn_keep(const mdn_shape *shape, const void *x, const mdn_kept *kept, void *stream);
+int mdn_kept_values(const mdn_shape *shape, const mdn_kept *kept, void *x, void *stream);
+int mdn_frontend_fwd_keep(const mdn_shape *shape, const void *x_q, const void *x_k, const void *x_v, const float *d, float eps, void *q, void *k,
+                          void *v, const mdn_kept *kept, void *stream);
+int mdn_frontend_fwd_kept(const mdn_shape *shape, const mdn_kept *kept, const float *d, float eps, void *q, void *k, void *v, void *stream);
+int mdn_frontend_bwd_kept(const mdn_shape *shape, const mdn_kept *kept, const float *d, float eps, const void *dq, const void *dk, const void *dv,
+                          void *dx_q, void *dx_k, void *dx_v, float *dd, void *workspace, size_t workspace_bytes, void *stream);
+int mdn_epilogue_fwd_keep(const mdn_shape *shape, const void *o, const void *g, const float *w, float eps, void *y, const mdn_kept *kept,
+                          void *stream);
+int mdn_epilogue_bwd_kept(const mdn_shape *shape, const mdn_kept *kept, const float *w, float eps, const void *dy, void *d_o, void *dg, float *dw,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Optional per-kernel timing (used by the benchmark to attribute time to kernels).
  * Between mdn_profile_begin() and mdn_profile_end() every kernel the library launches is
  * bracketed by a pair of HIP events recorded on the launch stream.  mdn_profile_end()

@@ -29,7 +29,9 @@ EXPORTS = ("mdn_version", "mdn_strerror", "mdn_workspace_bytes", "mdn_saved_stat
            "mdn_profile_launch_counts", "mdn_set_segments",
            "mdn_gates_fwd", "mdn_gates_bwd", "mdn_frontend_fwd", "mdn_frontend_bwd", "mdn_epilogue_fwd",
            "mdn_epilogue_bwd", "mdn_workspace_bytes_varlen", "mdn_chunk_fwd_varlen", "mdn_chunk_bwd_varlen",
-           "mdn_gdr_bytes", "mdn_gdr_chunk_fwd", "mdn_gdr_chunk_bwd", "mdn_gdr_recurrent_step")
+           "mdn_gdr_bytes", "mdn_gdr_chunk_fwd", "mdn_gdr_chunk_bwd", "mdn_gdr_recurrent_step",
+           "mdn_kept_workspace_bytes", "mdn_keep", "mdn_kept_values", "mdn_frontend_fwd_keep", "mdn_frontend_fwd_kept",
+           "mdn_frontend_bwd_kept", "mdn_epilogue_fwd_keep", "mdn_epilogue_bwd_kept")
 
 KERNEL_NAMES = ("intra_fwd", "scan_fwd", "intra_bwd", "rebuild", "scan_bwd", "grad", "recurrent")
 
@@ -48,6 +50,10 @@ class MdnGateParams(ctypes.Structure):
 class MdnGdrShape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("dk", ctypes.c_int32),
                 ("dv", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class MdnKept(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("exponents", ctypes.c_void_p)]
 
 
 class MdnError(RuntimeError):
@@ -124,6 +130,17 @@ def load_library():
     lib.mdn_gdr_chunk_bwd.argtypes = [gs, ip, ctypes.c_int32] + [vp] * 17 + [ctypes.c_size_t, vp]
     lib.mdn_gdr_recurrent_step.restype = ctypes.c_int
     lib.mdn_gdr_recurrent_step.argtypes = [gs] + [vp] * 8
+    kp, sz = ctypes.POINTER(MdnKept), ctypes.c_size_t
+    lib.mdn_kept_workspace_bytes.argtypes = [sp, ctypes.POINTER(sz)]
+    lib.mdn_keep.argtypes = [sp, vp, kp, vp]
+    lib.mdn_kept_values.argtypes = [sp, kp, vp, vp]
+    lib.mdn_frontend_fwd_keep.argtypes = [sp, vp, vp, vp, fp, cf, vp, vp, vp, kp, vp]
+    lib.mdn_frontend_fwd_kept.argtypes = [sp, kp, fp, cf, vp, vp, vp, vp]
+    lib.mdn_frontend_bwd_kept.argtypes = [sp, kp, fp, cf] + [vp] * 6 + [fp, vp, sz, vp]
+    lib.mdn_epilogue_fwd_keep.argtypes = [sp, vp, vp, fp, cf, vp, kp, vp]
+    lib.mdn_epilogue_bwd_kept.argtypes = [sp, kp, fp, cf, vp, vp, vp, fp, vp, sz, vp]
+    for name in EXPORTS[-8:]:
+        getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -313,3 +330,38 @@ def mdn_gdr_chunk_bwd(q, k, g, beta, e, dO, S0=None, states=None, operands=None,
 def mdn_gdr_recurrent_step(q, k, v, g, beta, S, scale=None, out=None):
     """Gated delta rule over the T tokens given, one after the other; S [B, H, dk, dv] fp32 is updated in place.  Returns o."""
     return (_host or _load_host()).gdr_recurrent_step(q, k, v, g, beta, S, scale, out)
+
+
+def mdn_keep(x):
+    """8-bit checkpoint of x [B, T, H, d] (d 64 or 128): a pair (codes int8 [B, T, H, d], exponents uint8 [B, T, H, d / 32])."""
+    return (_host or _load_host()).keep(x)
+
+
+def mdn_kept_values(kept, dtype):
+    """What a checkpoint reads back as, as torch.bfloat16 or torch.float32 (exact in either)."""
+    return (_host or _load_host()).kept_values(kept, dtype)
+
+
+def mdn_frontend_fwd_keep(x_q, x_k, x_v, d, eps=1e-6):
+    """mdn_frontend_fwd that also keeps its inputs in 8 bits -> dict(q, k, v, kept_q, kept_k, kept_v)."""
+    return (_host or _load_host()).frontend_fwd_keep(x_q, x_k, x_v, d, eps)
+
+
+def mdn_frontend_fwd_kept(kept_q, kept_k, kept_v, d, dtype, eps=1e-6):
+    """The front end from checkpoints -> dict(q, k, v) of the dtype asked for (what the rule's backward reads)."""
+    return (_host or _load_host()).frontend_fwd_kept(kept_q, kept_k, kept_v, d, dtype, eps)
+
+
+def mdn_frontend_bwd_kept(kept_q, kept_k, kept_v, d, dq, dk, dv, eps=1e-6, want_dd=True):
+    """Adjoint of the front end from checkpoints: dict(dx_q, dx_k, dx_v, dd [H] or None)."""
+    return (_host or _load_host()).frontend_bwd_kept(kept_q, kept_k, kept_v, d, dq, dk, dv, eps, want_dd)
+
+
+def mdn_epilogue_fwd_keep(o, g, w, eps=1e-6):
+    """mdn_epilogue_fwd that also keeps its inputs in 8 bits -> dict(y, kept_o, kept_g)."""
+    return (_host or _load_host()).epilogue_fwd_keep(o, g, w, eps)
+
+
+def mdn_epilogue_bwd_kept(kept_o, kept_g, w, dy, eps=1e-6, want_dw=True):
+    """Adjoint of the back end from checkpoints: dict(do, dg, dw [dv] or None)."""
+    return (_host or _load_host()).epilogue_bwd_kept(kept_o, kept_g, w, dy, eps, want_dw)

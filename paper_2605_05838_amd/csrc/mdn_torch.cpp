@@ -9,6 +9,7 @@
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -761,6 +762,221 @@ PyObject *epilogue_bwd(PyObject *const *x) {
     return r.release();
 }
 
+// ---- 8-bit checkpoints
+
+// a (codes, exponents) pair of a [B, T, H, d] tensor
+struct KeptPair {
+    const at::Tensor &codes, &exponents;
+    static PyObject *item(PyObject *o, int i, const char *name) {
+        if (!o || !PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) fail(std::string(name) + " must be a pair (codes, exponents)");
+        return PyTuple_GET_ITEM(o, i);
+    }
+    KeptPair(PyObject *o, const char *name) : codes(need(item(o, 0, name), name)), exponents(need(item(o, 1, name), name)) {
+        if (codes.dim() != 4 || codes.size(3) % 32) fail(std::string(name) + ": codes must be [B, T, H, d], d a multiple of 32; got " + str(codes.sizes()));
+        expect(name, &codes, {codes.size(0), codes.size(1), codes.size(2), codes.size(3)}, at::kChar, codes);
+        expect(name, &exponents, {codes.size(0), codes.size(1), codes.size(2), codes.size(3) / 32}, at::kByte, codes);
+    }
+    mdn_kept c() const { return mdn_kept{ptr<int8_t>(codes), ptr<uint8_t>(exponents)}; }
+    void like(const char *name, const KeptPair &o) const {
+        if (codes.sizes() != o.codes.sizes()) fail(std::string(name) + ": expected shape " + str(o.codes.sizes()) + ", got " + str(codes.sizes()));
+        if (codes.device() != o.codes.device()) fail(std::string(name) + ": all tensors of a call share one device");
+    }
+};
+// a new checkpoint like x
+struct NewKept {
+    at::Tensor codes, exponents;
+    explicit NewKept(const at::Tensor &x)
+        : codes(empty(x.sizes(), at::kChar, x)), exponents(empty({x.size(0), x.size(1), x.size(2), x.size(3) / 32}, at::kByte, x)) {}
+    mdn_kept c() const { return mdn_kept{ptr<int8_t>(codes), ptr<uint8_t>(exponents)}; }
+    PyObject *pair() const {
+        Ref a(THPVariable_Wrap(codes)), b(THPVariable_Wrap(exponents));
+        if (!a.p || !b.p) throw Fail{};
+        PyObject *t = PyTuple_Pack(2, a.p, b.p);
+        if (!t) throw Fail{};
+        return t;
+    }
+};
+void set_pair(Dict &r, const char *key, const NewKept &k) {
+    const Ref t(k.pair());
+    if (PyDict_SetItemString(r.d, key, t.p) < 0) throw Fail{};
+}
+mdn_shape rows_shape(const at::Tensor &x, int dtype) {
+    for (int64_t n : x.sizes())
+        if (n > 0x7fffffff) fail("sizes must fit 32 bits");
+    return mdn_shape{(int32_t)x.size(0), (int32_t)x.size(1), (int32_t)x.size(2), (int32_t)x.size(3), (int32_t)x.size(3), 64, dtype, 1.f};
+}
+// a torch.dtype argument
+at::ScalarType storage_type(PyObject *o) {
+    if (!THPDtype_Check(o)) fail("dtype must be torch.bfloat16 or torch.float32");
+    const at::ScalarType t = reinterpret_cast<THPDtype *>(o)->scalar_type;
+    if (t != at::kBFloat16 && t != at::kFloat) fail("dtype must be torch.bfloat16 or torch.float32");
+    return t;
+}
+int code_of(at::ScalarType t) { return t == at::kFloat ? MDN_DTYPE_F32 : MDN_DTYPE_BF16; }
+size_t kept_workspace(const mdn_shape &s) {
+    size_t n = 0;
+    check(mdn_kept_workspace_bytes(&s, &n), "mdn_kept_workspace_bytes");
+    return n;
+}
+// rows the front end's and back end's kernels take
+void expect_rows(const at::Tensor &x, const char *name) {
+    if (x.dim() != 4 || (x.size(3) != 64 && x.size(3) != 128)) fail(std::string(name) + " must be [B, T, H, d], d 64 or 128; got " + str(x.sizes()));
+}
+
+// x
+PyObject *keep(PyObject *const *x) {
+    const at::Tensor &t = need(x[0], "x");
+    expect_rows(t, "x");
+    const mdn_shape s = rows_shape(t, dtype_code(t));
+    expect("x", &t, {t.size(0), t.size(1), t.size(2), t.size(3)}, t.scalar_type(), t);
+    const OnDevice dev(t);
+    const NewKept k(t);
+    const mdn_kept c = k.c();
+    call("mdn_keep", mdn_keep, &s, ptr(t), &c, dev.stream);
+    return k.pair();
+}
+
+// kept dtype
+PyObject *kept_values(PyObject *const *x) {
+    const KeptPair k(x[0], "kept");
+    expect_rows(k.codes, "kept");
+    const at::ScalarType dt = storage_type(x[1]);
+    const mdn_shape s = rows_shape(k.codes, code_of(dt));
+    const OnDevice dev(k.codes);
+    at::Tensor t = empty(k.codes.sizes(), dt, k.codes);
+    const mdn_kept c = k.c();
+    call("mdn_kept_values", mdn_kept_values, &s, &c, ptr(t), dev.stream);
+    return THPVariable_Wrap(t);
+}
+
+// x_q x_k x_v d eps
+PyObject *frontend_fwd_keep(PyObject *const *x) {
+    const FrontInputs in(x);
+    expect_rows(in.q, "x_q");
+    expect("x_v", &in.v, {in.q.size(0), in.q.size(1), in.q.size(2), in.q.size(3)}, in.dt, in.q);
+    const double eps = number(x[4]);
+    const OnDevice dev(in.q);
+    at::Tensor q = empty(in.q.sizes(), in.dt, in.q), k = empty(in.k.sizes(), in.dt, in.q), v = empty(in.v.sizes(), in.dt, in.q);
+    const NewKept kq(in.q), kk(in.k), kv(in.v);
+    const mdn_kept c[3] = {kq.c(), kk.c(), kv.c()};
+    call("mdn_frontend_fwd_keep", mdn_frontend_fwd_keep, &in.s, ptr(in.q), ptr(in.k), ptr(in.v), ptr<float>(in.d), (float)eps, ptr(q), ptr(k), ptr(v),
+         static_cast<const mdn_kept *>(c), dev.stream);
+    Dict r;
+    r.set("q", q);
+    r.set("k", k);
+    r.set("v", v);
+    set_pair(r, "kept_q", kq);
+    set_pair(r, "kept_k", kk);
+    set_pair(r, "kept_v", kv);
+    return r.release();
+}
+
+// kept_q kept_k kept_v d of the front end
+struct FrontKept {
+    const KeptPair q, k, v;
+    const at::Tensor &d;
+    mdn_kept c[3];
+    explicit FrontKept(PyObject *const *x) : q(x[0], "kept_q"), k(x[1], "kept_k"), v(x[2], "kept_v"), d(need(x[3], "d")), c{q.c(), k.c(), v.c()} {
+        expect_rows(q.codes, "kept_q");
+        k.like("kept_k", q);
+        v.like("kept_v", q);
+        expect("d", &d, {q.codes.size(2)}, at::kFloat, q.codes);
+    }
+};
+
+// kept_q kept_k kept_v d dtype eps
+PyObject *frontend_fwd_kept(PyObject *const *x) {
+    const FrontKept in(x);
+    const at::ScalarType dt = storage_type(x[4]);
+    const double eps = number(x[5]);
+    const mdn_shape s = rows_shape(in.q.codes, code_of(dt));
+    const OnDevice dev(in.q.codes);
+    const at::IntArrayRef n = in.q.codes.sizes();
+    at::Tensor q = empty(n, dt, in.q.codes), k = empty(n, dt, in.q.codes), v = empty(n, dt, in.q.codes);
+    call("mdn_frontend_fwd_kept", mdn_frontend_fwd_kept, &s, static_cast<const mdn_kept *>(in.c), ptr<float>(in.d), (float)eps, ptr(q), ptr(k), ptr(v),
+         dev.stream);
+    Dict r;
+    r.set("q", q);
+    r.set("k", k);
+    r.set("v", v);
+    return r.release();
+}
+
+// kept_q kept_k kept_v d dq dk dv eps want_dd
+PyObject *frontend_bwd_kept(PyObject *const *x) {
+    const FrontKept in(x);
+    const at::Tensor &dq = need(x[4], "dq"), &dk = need(x[5], "dk"), &dv = need(x[6], "dv"), &like = in.q.codes;
+    const at::ScalarType dt = dq.scalar_type();
+    const mdn_shape s = rows_shape(like, dtype_code(dq));
+    expect("dq", &dq, {s.B, s.T, s.H, s.dk}, dt, like);
+    expect("dk", &dk, {s.B, s.T, s.H, s.dk}, dt, like);
+    expect("dv", &dv, {s.B, s.T, s.H, s.dk}, dt, like);
+    const double eps = number(x[7]);
+    const OnDevice dev(like);
+    at::Tensor q = empty(like.sizes(), dt, like), k = empty(like.sizes(), dt, like), v = empty(like.sizes(), dt, like);
+    c10::optional<at::Tensor> dd, ws;
+    const size_t need_ws = kept_workspace(s);
+    if (truth(x[8])) {
+        dd = empty(in.d.sizes(), at::kFloat, like);
+        ws = bytes(need_ws, like);
+    }
+    call("mdn_frontend_bwd_kept", mdn_frontend_bwd_kept, &s, static_cast<const mdn_kept *>(in.c), ptr<float>(in.d), (float)eps, ptr(dq), ptr(dk), ptr(dv),
+         ptr(q), ptr(k), ptr(v), ptr<float>(dd), ptr(ws), ws ? need_ws : 0, dev.stream);
+    Dict r;
+    r.set("dx_q", q);
+    r.set("dx_k", k);
+    r.set("dx_v", v);
+    r.set("dd", dd);
+    return r.release();
+}
+
+// o g w eps
+PyObject *epilogue_fwd_keep(PyObject *const *x) {
+    const BackInputs in(x);
+    expect_rows(in.o, "o");
+    const double eps = number(x[3]);
+    const OnDevice dev(in.o);
+    at::Tensor y = empty(in.o.sizes(), in.dt, in.o);
+    const NewKept ko(in.o), kg(in.g);
+    const mdn_kept c[2] = {ko.c(), kg.c()};
+    call("mdn_epilogue_fwd_keep", mdn_epilogue_fwd_keep, &in.s, ptr(in.o), ptr(in.g), ptr<float>(in.w), (float)eps, ptr(y),
+         static_cast<const mdn_kept *>(c), dev.stream);
+    Dict r;
+    r.set("y", y);
+    set_pair(r, "kept_o", ko);
+    set_pair(r, "kept_g", kg);
+    return r.release();
+}
+
+// kept_o kept_g w dy eps want_dw
+PyObject *epilogue_bwd_kept(PyObject *const *x) {
+    const KeptPair o(x[0], "kept_o"), g(x[1], "kept_g");
+    const at::Tensor &w = need(x[2], "w"), &dy = need(x[3], "dy"), &like = o.codes;
+    expect_rows(like, "kept_o");
+    g.like("kept_g", o);
+    const at::ScalarType dt = dy.scalar_type();
+    const mdn_shape s = rows_shape(like, dtype_code(dy));
+    expect("w", &w, {s.dv}, at::kFloat, like);
+    expect("dy", &dy, {s.B, s.T, s.H, s.dv}, dt, like);
+    const double eps = number(x[4]);
+    const OnDevice dev(like);
+    at::Tensor d_o = empty(like.sizes(), dt, like), dg = empty(like.sizes(), dt, like);
+    c10::optional<at::Tensor> dw, ws;
+    const size_t need_ws = kept_workspace(s);
+    if (truth(x[5])) {
+        dw = empty(w.sizes(), at::kFloat, like);
+        ws = bytes(need_ws, like);
+    }
+    const mdn_kept c[2] = {o.c(), g.c()};
+    call("mdn_epilogue_bwd_kept", mdn_epilogue_bwd_kept, &s, static_cast<const mdn_kept *>(c), ptr<float>(w), (float)eps, ptr(dy), ptr(d_o), ptr(dg),
+         ptr<float>(dw), ptr(ws), ws ? need_ws : 0, dev.stream);
+    Dict r;
+    r.set("do", d_o);
+    r.set("dg", dg);
+    r.set("dw", dw);
+    return r.release();
+}
+
 template <PyObject *(*F)(PyObject *const *), int N> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n != N) {
         PyErr_Format(PyExc_TypeError, "expected %d arguments, got %zd", N, n);
@@ -796,6 +1012,8 @@ PyMethodDef methods[] = {MDN_ENTRY(chunk_fwd, 17), MDN_ENTRY(chunk_fwd_noalloc, 
                          MDN_ENTRY(gates_fwd, 11), MDN_ENTRY(gates_bwd, 16), MDN_ENTRY(frontend_fwd, 5),
                          MDN_ENTRY(frontend_bwd, 9), MDN_ENTRY(epilogue_fwd, 4), MDN_ENTRY(epilogue_bwd, 6),
                          MDN_ENTRY(gdr_chunk_fwd, 14), MDN_ENTRY(gdr_chunk_bwd, 15), MDN_ENTRY(gdr_recurrent_step, 8),
+                         MDN_ENTRY(keep, 1), MDN_ENTRY(kept_values, 2), MDN_ENTRY(frontend_fwd_keep, 5), MDN_ENTRY(frontend_fwd_kept, 6),
+                         MDN_ENTRY(frontend_bwd_kept, 9), MDN_ENTRY(epilogue_fwd_keep, 4), MDN_ENTRY(epilogue_bwd_kept, 6),
                          {"set_error_types", set_error_types, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mdn_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
