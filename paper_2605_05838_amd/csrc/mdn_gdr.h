@@ -191,6 +191,38 @@ template <typename T> __device__ __forceinline__ f32x4 gd_mma(typename Gd<T>::Fr
     return Op<T>::mma(a, b, c);
 }
 
+// A lane's reads of such a tile, as few byte offsets that are formed once: what the permutation adds depends on the lane and on the step (rows
+// as rows) or on the 32-column part (rows as contraction) alone, everything else is a constant of the instruction.
+template <typename T, int D> struct TileReader {
+    typedef Gd<T> G;
+    typedef typename G::Frag Frag;
+    static constexpr int NR = D / G::KS, NC = sizeof(T) == 2 ? D / 32 : 1;
+    unsigned ro[NR], co[NC];
+    int r, kg;
+    __device__ __forceinline__ TileReader(int r_, int kg_) : r(r_), kg(kg_) {
+        const T *z = nullptr;
+#pragma unroll
+        for (int s = 0; s < NR; ++s) ro[s] = (unsigned)(size_t)GTile<T, D>::at(z, G::row(0, r), (s * 4 + kg) * G::E);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int p = 0; p < NC; ++p) co[p] = (unsigned)(size_t)GTile<T, D>::at(z, 8 * kg + (r >> 2), 32 * p + 8 * (r & 3));
+        }
+    }
+    // GTile::row_frag of row Gd::row(t, r)
+    __device__ __forceinline__ Frag row_frag(const T *tile, int t, int s) const {
+        return *reinterpret_cast<const Frag *>(reinterpret_cast<const char *>(tile) + ro[s] + G::row(t, 0) * D * (int)sizeof(T));
+    }
+    // GTile::col_frag
+    __device__ __forceinline__ Frag col_frag(const T *tile, int t, int s) const {
+        if constexpr (sizeof(T) == 2) {
+            const bf16_t *p = reinterpret_cast<const bf16_t *>(reinterpret_cast<const char *>(tile) + co[t >> 1] + (32 * s * D + 4 * (t & 1)) * 2);
+            return tr_pair(p, p + 4 * D);
+        } else {
+            return GTile<T, D>::col_frag(tile, t, s, r, kg);
+        }
+    }
+};
+
 // one (sequence, value head) pair of a scan
 struct GdrSeq {
     size_t v, k;  // its first token as a row of the [tokens, H] and [tokens, Hk] tensors

@@ -1,17 +1,19 @@
 // What the forward and the reverse scan of the gated delta rule have in common.
 //
-// A workgroup walks the chunks of one (sequence, value head) pair for 32 columns of the state, one barrier per chunk, with six waves:
-//   waves 2, 3  the chain: 16 columns each, the state in their accumulators (see mdn_gdr.h);
-//   waves 0, 1  what hangs on the chain without being part of it, for the same columns, and every store;
-//   waves 4, 5  loads: the chunks ahead, HBM -> LDS without registers, into rings of kDepth chunks.
-// (Waves are dealt to the four SIMDs in turn: the chain has SIMDs 2 and 3 to itself.)  The fragments of T and P go from memory straight
-// into the registers of the one wave per 16 columns that wants them, asked for as soon as those of the chunk before are used up.
+// A workgroup walks the chunks of one (sequence, value head) pair for NCG groups of 16 columns of the state, one step per chunk, with
+// three kinds of waves (in this order: dealt to the four SIMDs in turn, the chain shares its own with the loads at most):
+//   2 waves     beside the chain: what hangs on it without being part of it, and every store;
+//   NCG waves   the chain: 16 columns each, the state in their accumulators (see mdn_gdr.h);
+//   2 waves     loads: the chunks ahead, HBM -> LDS without registers, into rings.
+// The chain itself takes 640 clocks a step at d = 128, the products' time; everything else must stay out of its way.  So it loads nothing: the
+// fragments of T, asked for by the wave that wants them as soon as those of the chunk before were used up, came back 2 000 clocks later, behind
+// all of the step's tiles, and were what a step waited for (2 050 clocks, and 4 100 with the remainders of T).  A chunk's tiles take 1 300 clocks
+// and more from the request to the last line, so that two chunks are on their way while one is worked on: rings of three (of two: 2 350 clocks a
+// step where three take 1 340).
 #pragma once
 #include "mdn_gdr.h"
 
 namespace mdn {
-
-constexpr int kGdrThreads = 384, kGdrCols = 32;
 
 // The tiles of a chunk that the loading waves (w2 = 0, 1) bring: [64][D] rows, permuted as GTile<T, LAYOUT> says
 template <typename T, int D, bool PERMUTED> struct GLoad {
@@ -31,19 +33,22 @@ template <typename T, int D, bool PERMUTED> struct GLoad {
     }
 };
 
-// A wave's triangle fragments of one chunk
-template <typename T> struct Triangle {
-    typename Gd<T>::Frag f[Gd<T>::NF];
-    __device__ __forceinline__ void load(const void *base, size_t blk, int lane) {
-        const auto *p = static_cast<const typename Gd<T>::Frag *>(base) + blk * (Gd<T>::NF * 64) + lane;
-#pragma unroll
-        for (int i = 0; i < Gd<T>::NF; ++i) f[i] = p[i * 64];
-    }
-};
-template <typename T, bool ON> struct TriangleIf : Triangle<T> {};
-template <typename T> struct TriangleIf<T, false> {
-    __device__ __forceinline__ void load(const void *, size_t, int) {}
-};
+// A triangle's fragments of one chunk (or 1 KB of coefficients): memory -> LDS as they lie there
+template <int BYTES> __device__ __forceinline__ void load_block(const void *base, size_t blk, void *to, int w2, int lane) {
+    const char *p = static_cast<const char *>(base) + blk * BYTES;
+    for (int u = w2; u < BYTES / 1024; u += 2) dma16(p, u * 1024 + lane * 16, lds_addr(to) + u * 1024);
+}
+
+// Everything asked for so far is there, and the compiler knows: it otherwise waits inside a loop for what was requested in front of it.
+__device__ __forceinline__ void all_arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); } // vmcnt(0)
+
+// the slot of a ring of N that step n + 1 uses after step n's
+template <int N> __device__ __forceinline__ int next_slot(int s) { return s + 1 == N ? 0 : s + 1; }
+
+// fragment i of a triangle in LDS
+template <typename T> __device__ __forceinline__ typename Gd<T>::Frag tri_frag(const T *tri, int i, int lane) {
+    return *reinterpret_cast<const typename Gd<T>::Frag *>(tri + (i * 64 + lane) * Gd<T>::E);
+}
 
 // B fragments of N accumulator tiles, with their remainders (PRECISE)
 template <typename T, int N, bool PRECISE> struct Frags {
@@ -75,37 +80,69 @@ template <typename T, int N> struct Slate {
     }
 };
 
-// a slate of 64 tokens -> 16 columns of `rows` rows of a [tokens, H, dv] tensor
-template <typename T> __device__ __forceinline__ void store_tokens(T *base, unsigned rs, const T *slate, int rows, int r, int kg) {
-    constexpr int LD = Slate<T, 64>::LD;
+// Stores of the waves beside the chain go through buffer descriptors: what lies behind the last row, and a tensor that is not wanted (no
+// bytes in reach), is dropped by the bounds check.  With branches around them the compiler cannot count what is on its way behind the
+// loads it waits for, and waits for all of it.
+typedef unsigned gdr_u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t out_rows(void *base, size_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(base, 0, (int)bytes, 0x00020000);
+}
+template <int AUX, typename V> __device__ __forceinline__ void put16(__amdgpu_buffer_rsrc_t to, unsigned at, V v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(gdr_u32x4, v), to, at, 0, AUX);
+}
+
+// NG slates of LD rows, one after the other -> 32 tokens from token t0 on of a chunk of a [tokens, H, dv] tensor (`to`: from its first
+// row and the first of the 16 NG columns on; rs: bytes between rows), whole rows of these columns at a time (32 bytes of a row and, later,
+// the other 32 cost HBM two writes)
+template <typename T, int NG, int LD>
+__device__ __forceinline__ void store_tokens(__amdgpu_buffer_rsrc_t to, unsigned rs, const T *slates, int slate_t0, int t0, int r, int kg) {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const auto v = column4(slate, LD, 4 * kg, 16 * i, r);
-        const int tok = 16 * i + r;
-        if (tok < rows) __builtin_nontemporal_store(v, reinterpret_cast<decltype(column4(slate, LD, 0, 0, 0)) *>(at32(base, tok * rs + 4 * kg)));
+        for (int i = 0; i < NG; ++i) {
+            const int pc = NG == 2 ? kg : kg & 1, tok = 16 * (NG == 2 ? i : kg >> 1) + r; // 16-byte piece of the row, token
+            const T *p = slates + (8 * pc + (r >> 2)) * LD + slate_t0 + tok - r + 4 * (r & 3);
+            put16<2>(to, (unsigned)(t0 + tok) * rs + 16 * pc, tr_pair(p, p + 4 * LD));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int pc = kg; pc < 4 * NG; pc += 4)
+                put16<2>(to, (unsigned)(t0 + 16 * i + r) * rs + 16 * pc, column4(slates, LD, 4 * pc, slate_t0 + 16 * i, r));
     }
 }
 
-// A slate of DK rows of a state -> a chunk block of kept states: A fragments (row tile t, step of dv), [dv / KS][DK / 16] of them,
-// cg: the 16-column group of the workgroup, col0: the workgroup's first column
-template <typename T, int DK> __device__ __forceinline__ void store_state(T *block, const T *slate, int cg, int col0, int lane) {
+// NG slates of DK rows of a state, 16 columns each from column `col` on -> a chunk block of kept states: A fragments (row tile t, step of
+// dv), [dv / KS][DK / 16] of them.  By two waves (w = 0, 1).
+template <typename T, int DK, int NG>
+__device__ __forceinline__ void store_state(__amdgpu_buffer_rsrc_t block, const T (&slates)[NG][Slate<T, DK>::SIZE], int w, int col, int lane) {
     constexpr int LD = Slate<T, DK>::LD, NT = DK / 16;
-    if constexpr (sizeof(T) == 2) { // two lane groups per tile: the other two are the other 16 columns'
-        const int r = lane & 15, g = lane >> 4 & 1, up = lane >> 5;
+    const int r = lane & 15, kg = lane >> 4;
+    if constexpr (sizeof(T) == 2 && NG == 2) { // whole fragments, every other one
+        const T *p = slates[0] + (8 * kg + (r >> 2)) * LD + 8 * (r & 3); // (the second slate's columns are rows 16 ..: one after the other)
 #pragma unroll
         for (int tt = 0; tt < NT; tt += 2) {
-            const int t = tt + up, dk = 32 * (t >> 1) + 4 * (t & 1) + 8 * (r & 3);
-            const bf16_t *p = slate + (8 * g + (r >> 2)) * LD + dk;
-            const bf16x8 v = tr_pair(p, p + 4 * LD);
-            __builtin_nontemporal_store(v, reinterpret_cast<bf16x8 *>(block + (((size_t)(col0 >> 5) * NT + t) * 64 + (2 * cg + g) * 16 + r) * 8));
+            const int t = tt + w;
+            const T *x = p + 32 * (t >> 1) + 4 * (t & 1);
+            put16<2>(block, (unsigned)((((col >> 5) * NT + t) * 64 + lane) * 16), tr_pair(x, x + 4 * LD));
+        }
+    } else if constexpr (sizeof(T) == 2) { // half of every fragment: two lane groups per tile
+        const int g = kg & 1, half = col >> 3 & 2;
+        const T *p = slates[0] + (8 * g + (r >> 2)) * LD + 8 * (r & 3);
+#pragma unroll
+        for (int tt = 0; tt < NT; tt += 4) {
+            const int t = tt + 2 * w + (kg >> 1);
+            const T *x = p + 32 * (t >> 1) + 4 * (t & 1);
+            put16<2>(block, (unsigned)((((col >> 5) * NT + t) * 64 + (half + g) * 16 + r) * 16), tr_pair(x, x + 4 * LD));
         }
     } else {
-        const int r = lane & 15, kg = lane >> 4;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const f32x4 v = column4(slate, LD, 4 * kg, 16 * t, r);
-            __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(block + (((size_t)(col0 / 16 + cg) * NT + t) * 64 + lane) * 4));
-        }
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int tt = 0; tt < NT; tt += 2) {
+                const int t = tt + w;
+                put16<2>(block, (unsigned)((((col / 16 + g) * NT + t) * 64 + lane) * 16), column4(slates[g], LD, 4 * kg, 16 * t, r));
+            }
     }
 }
 
@@ -122,5 +159,8 @@ template <typename T, int NT> __device__ __forceinline__ void save_state(const f
 #pragma unroll
         for (int x = 0; x < 4; ++x) g[(size_t)(Gd<T>::row(t, 4 * kg) + x) * dv + col + r] = S[t][x];
 }
+
+// 16 columns per workgroup while the CUs hold all of those workgroups, or 32
+inline bool gdr_one_group(const GdrDims &d) { return (long long)(d.B * d.H + 7) / 8 * 8 * (d.dv / 16) <= num_cus(); }
 
 } // namespace mdn

@@ -1,6 +1,8 @@
 // Gated delta rule, reverse scan.  Per chunk, D the adjoint of the state at its END, from the last chunk to the first, dO' = scale dO:
-//     beside the chain, one chunk ahead (waves 0, 1):   X = P^T dO',   Y = (e^G Q)^T dO'   (fp32, through LDS); stores of dV and D
-//     chain (waves 2, 3):   dE = X + e^{G_C - G} beta K D,   dV = T^T dE,   D <- e^{G_C} D + Y - K^T (e^G dV)
+//     beside the chain, one chunk ahead:   X = P^T dO',   Y = (e^G Q)^T dO'   (fp32, through LDS); stores of dV and D
+//     chain:   dE = X + e^{G_C - G} beta K D,   dV = T^T dE,   D <- e^{G_C} D + Y - K^T (e^G dV)
+// Two barriers a step: at its start, and when the chain has taken X and Y and the waves beside it have taken the step before's D and dV:
+// then either side writes the next.
 // PRECISE (a call that asks for dS0, which is 32-bit): as in the forward scan; P^T and e^G dO' have remainders as well (dO and Q are exact).
 #include "mdn_gdr_scan.h"
 
@@ -8,34 +10,36 @@ namespace mdn {
 
 namespace {
 
-template <typename T, int DK, bool PRECISE>
-__global__ __launch_bounds__(kGdrThreads) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
+template <typename T, int DK, int NCG, bool PRECISE>
+__global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
     typedef Gd<T> G;
-    typedef GTile<T, DK> Tile;
+    typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
     typedef Slate<T, 64> SlateE;
-    constexpr int NT = DK / 16, SK = DK / G::KS, S64 = 64 / G::KS;
-    constexpr bool RING = sizeof(T) == 2; // otherwise loads between two barriers, not beside the products
-    constexpr int D = RING ? 3 : 1, DQ = RING ? 2 : 1, DC = 3;
+    constexpr int NT = DK / 16, SK = DK / G::KS, S64 = 64 / G::KS, COLS = 16 * NCG, TRI = G::NF * 64 * G::E;
+    constexpr int TB = TRI * (int)sizeof(T); // bytes of a triangle
+    constexpr bool RING = sizeof(T) == 2;    // otherwise loads between two barriers, not beside the products
+    // ring depths: what the chain reads; T^T; what the waves beside it read (there is no room for three of everything); coefficients
+    constexpr int D = RING ? 3 : 1, DT = PRECISE ? 2 : D, DQ = RING ? 2 : 1, DC = 4;
+    constexpr int SETS = RING ? 2 : 1; // chunks of P^T that a wave beside the chain has asked for
     typedef GLoad<T, DK, true> LoadK;
-    typedef GLoad<T, kGdrCols, false> LoadV;
-    __shared__ __align__(16) T s_k[D][64 * DK], s_q[DQ][64 * DK], s_do[DQ][64 * kGdrCols];
+    typedef GLoad<T, COLS, false> LoadV;
+    __shared__ __align__(16) T s_k[D][64 * DK], s_q[DQ][64 * DK], s_do[DQ][64 * COLS], s_t[DT][TRI], s_tl[DT][PRECISE ? TRI : 8];
     __shared__ __align__(16) float s_c[DC][kGdrCoef];
-    __shared__ __align__(16) f32x4 s_x[2][4][64], s_y[2][NT][64];
-    __shared__ __align__(16) T s_s[2][2][SlateS::SIZE], s_r[2][2][SlateE::SIZE];
+    __shared__ __align__(16) f32x4 s_x[NCG][4][64], s_y[NCG][NT][64];
+    __shared__ __align__(16) T s_s[NCG][SlateS::SIZE], s_r[NCG * SlateE::SIZE];
 
     const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, kg = lane >> 4;
     int bh, sub;
-    xcd_map(first + (int)blockIdx.x, d.dv / kGdrCols, bh, sub);
+    xcd_map(first + (int)blockIdx.x, d.dv / COLS, bh, sub);
     if (bh >= d.B * d.H) return;
     const GdrSeq q = gdr_seq(d, bh);
-    const int col0 = sub * kGdrCols, N = q.n, last = (q.len - 1) & 63; // last: the last row of the last chunk
+    const int col0 = sub * COLS, N = q.n, last = (q.len - 1) & 63; // last: the last row of the last chunk
     const unsigned rsv = (unsigned)(d.H * d.dv), rsk = (unsigned)(d.Hk * DK);
 
-    // Step n: chunk N - 1 - n on the chain, the one before it (in time) beside it.  Barriers of a step: at its start; when the chain has
-    // taken X and Y; without a ring also at its end.
-    if (w >= 4) { // ---- loads
-        const int w2 = w - 4;
+    // Step n: chunk N - 1 - n on the chain, the one before it (in time) beside it
+    if (w >= 2 + NCG) { // ---- loads
+        const int w2 = w - 2 - NCG;
         LoadK lk, lk_end;
         LoadV lv, lv_end;
         const T *k = static_cast<const T *>(a.k) + q.k * DK, *qq = static_cast<const T *>(a.q) + q.k * DK;
@@ -45,33 +49,47 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_bwd_kernel(GdrDims d, Gd
         lk_end.aim(rsk, w2, lane, last);
         lv_end.aim(rsv, w2, lane, last);
         auto get_k = [&](int n) { (n == 0 ? lk_end : lk).request(k + (size_t)(N - 1 - n) * 64 * rsk, s_k[n % D], w2); };
+        auto get_t = [&](int n) {
+            load_block<TB>(a.TT, q.blk + (N - 1 - n), s_t[n % DT], w2, lane);
+            if constexpr (PRECISE) load_block<TB>(a.TT_lo, q.blk + (N - 1 - n), s_tl[n % DT], w2, lane);
+        };
         auto get_q = [&](int n) {
-            (n == 0 ? lk_end : lk).request(qq + (size_t)(N - 1 - n) * 64 * rsk, s_q[n % DQ], w2);
-            (n == 0 ? lv_end : lv).request(v + (size_t)(N - 1 - n) * 64 * rsv, s_do[n % DQ], w2);
-            if (w2 == 0) dma16(a.coef + (q.blk + (N - 1 - n)) * kGdrCoef, lane * 16, lds_addr(s_c[n % DC]));
+            const int m = N - 1 - n;
+            if (w2 == 0) dma16(a.coef + (q.blk + m) * kGdrCoef, lane * 16, lds_addr(s_c[n % DC]));
+            (n == 0 ? lk_end : lk).request(qq + (size_t)m * 64 * rsk, s_q[n % DQ], w2);
+            (n == 0 ? lv_end : lv).request(v + (size_t)m * 64 * rsv, s_do[n % DQ], w2);
         };
         get_q(0);
+        wait_vm<0>();
+        __syncthreads();
         if constexpr (RING) {
             get_k(0);
+            get_t(0);
             if (N > 1) {
                 get_q(1);
                 get_k(1);
+                if (DT == D) get_t(1);
             }
+            wait_vm<0>();
         }
-        wait_vm<0>();
-        __syncthreads();
         __syncthreads();
         for (int n = 0; n <= N; ++n) {
             if constexpr (RING) {
                 __syncthreads();
+                if (DT < D && n + 1 < N) get_t(n + 1);
                 if (n + 2 < N) {
                     get_q(n + 2); // (for step n + 1)
                     get_k(n + 2);
+                    if (DT == D) get_t(n + 2);
                 }
                 __syncthreads();
-                n + 2 < N ? wait_vm<LoadK::COUNT>() : wait_vm<0>();
+                // (the last ones asked for are those of step n + 2)
+                n + 2 < N ? wait_vm<LoadK::COUNT + (DT == D ? TB / 2048 : 0)>() : wait_vm<0>();
             } else {
-                if (n < N) get_k(n);
+                if (n < N) {
+                    get_k(n);
+                    get_t(n);
+                }
                 if (n + 1 < N) get_q(n + 1);
                 wait_vm<0>();
                 __syncthreads();
@@ -82,40 +100,51 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_bwd_kernel(GdrDims d, Gd
         return;
     }
 
-    const int cg = w & 1, col = col0 + 16 * cg;
+    const TileReader<T, DK> tile(r, kg);
     if (w >= 2) { // ---- the chain
-        Triangle<T> tri;
-        TriangleIf<T, PRECISE> tri_lo;
-        tri.load(a.TT, q.blk + N - 1, lane);
-        tri_lo.load(a.TT_lo, q.blk + N - 1, lane);
+        const int cg = w - 2, col = col0 + 16 * cg;
+        int slot = 0, slot_t = 0, slot_c = 0;
         f32x4 S[NT];
         load_state<T>(S, a.dS_final ? a.dS_final + q.state * DK * d.dv : nullptr, d.dv, col, r, kg);
+        all_arrived();
         __syncthreads();
         __syncthreads();
         for (int n = 0; n <= N; ++n) {
             __syncthreads();
             if (n < N) {
-                const T *k = s_k[n % D];
-                const float *c = s_c[n % DC];
-                f32x4 X[4];
+                const T *k = s_k[slot], *tri = s_t[slot_t], *tri_lo = s_tl[slot_t];
+                const float *c = s_c[slot_c] + G::row(0, 4 * kg);
+                f32x4 X[4], eg[4], ec[4];
+                auto decays = [&] {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        eg[t] = *reinterpret_cast<const f32x4 *>(c + G::row(t, 0));
+                        ec[t] = *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 0));
+                    }
+                };
+                if (RING) decays(); // (32-bit storage has no registers for them yet)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) X[t] = s_x[cg][t][lane];
                 Frags<T, NT, PRECISE> Sb;
                 Sb.from(S);
-                const float eC = c[63];
+                const float eC = s_c[slot_c][63];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) S[t] = eC * S[t] + s_y[cg][t][lane];
                 __syncthreads();
 #pragma unroll
-                for (int s = 0; s < SK; ++s) SlateS::put(s_s[n & 1][cg], s, r, kg, Sb.hi[s]);
+                for (int s = 0; s < SK; ++s) SlateS::put(s_s[cg], s, r, kg, Sb.hi[s]);
                 f32x4 E[4];
                 zero_acc(E);
 #pragma unroll
                 for (int s = 0; s < SK; ++s)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) E[t] = Sb.mma(Tile::row_frag(k, G::row(t, r), s, kg), s, E[t]);
+                    for (int t = 0; t < 4; ++t) E[t] = Sb.mma(tile.row_frag(k, t, s), s, E[t]);
+                if (!RING) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    decays();
+                }
 #pragma unroll
-                for (int t = 0; t < 4; ++t) E[t] = X[t] + *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 4 * kg)) * E[t];
+                for (int t = 0; t < 4; ++t) E[t] = X[t] + ec[t] * E[t];
                 Frags<T, 4, PRECISE> Eb;
                 Eb.from(E);
                 f32x4 R[4];
@@ -125,23 +154,22 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_bwd_kernel(GdrDims d, Gd
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
                         if (s >= G::first(t)) {
-                            R[t] = Eb.mma(tri.f[G::up(t, s)], s, R[t]);
-                            if constexpr (PRECISE) R[t] = gd_mma<T>(tri_lo.f[G::up(t, s)], Eb.hi[s], R[t]);
+                            R[t] = Eb.mma(tri_frag(tri, G::up(t, s), lane), s, R[t]);
+                            if constexpr (PRECISE) R[t] = gd_mma<T>(tri_frag(tri_lo, G::up(t, s), lane), Eb.hi[s], R[t]);
                         }
-                if (n + 1 < N) {
-                    tri.load(a.TT, q.blk + N - 2 - n, lane);
-                    tri_lo.load(a.TT_lo, q.blk + N - 2 - n, lane);
-                }
 #pragma unroll
-                for (int s = 0; s < S64; ++s) SlateE::put(s_r[n & 1][cg], s, r, kg, G::frag(&R[s * G::KT]));
+                for (int s = 0; s < S64; ++s) SlateE::put(s_r + cg * SlateE::SIZE, s, r, kg, G::frag(&R[s * G::KT]));
 #pragma unroll
-                for (int t = 0; t < 4; ++t) R[t] *= -*reinterpret_cast<const f32x4 *>(c + G::row(t, 4 * kg));
+                for (int t = 0; t < 4; ++t) R[t] *= -eg[t];
                 Frags<T, 4, PRECISE> Rb;
                 Rb.from(R);
 #pragma unroll
                 for (int s = 0; s < S64; ++s)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) S[t] = Rb.mma(Tile::col_frag(k, t, s, r, kg), s, S[t]);
+                    for (int t = 0; t < NT; ++t) S[t] = Rb.mma(tile.col_frag(k, t, s), s, S[t]);
+                slot = next_slot<D>(slot);
+                slot_t = next_slot<DT>(slot_t);
+                slot_c = next_slot<DC>(slot_c);
             } else {
                 __syncthreads();
             }
@@ -151,77 +179,128 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_bwd_kernel(GdrDims d, Gd
         return;
     }
 
-    // ---- beside the chain
-    Triangle<T> tri;
-    TriangleIf<T, PRECISE> tri_lo;
-    auto get_tri = [&](int n) {
-        tri.load(a.PT, q.blk + N - 1 - n, lane);
-        tri_lo.load(a.PT_lo, q.blk + N - 1 - n, lane);
-    };
-    if (RING) get_tri(0); // (32-bit storage: 40 registers, which are not there between the uses)
-    f32x4 X[4], Y[NT];
-    auto ahead = [&](int n) { // X, Y of step n
-        const T *qt = s_q[n % DQ], *dO = s_do[n % DQ];
-        const float *c = s_c[n % DC];
-        const int rows = n == 0 ? last + 1 : 64;
-        if (!RING) get_tri(n);
-        zero_acc(X);
+    // ---- beside the chain: X of 32 tokens, Y of half of dk, all columns.  The wave's fragments of P^T are nobody else's and come straight
+    // into registers, SETS chunks ahead.
+    auto beside = [&](auto first_tile) {
+        constexpr int T0 = decltype(first_tile)::value, HT = NT / 2;
+        struct Set { Frag p[2][S64], lo[2][PRECISE ? S64 : 1]; } sets[SETS];
+        int slot = 0, slot_c = 0;
+        auto fetch = [&](Set &x, int n) {
+            n = min(n, N - 1); // (asked for again behind the last chunk: no branch around loads in flight)
+            const size_t at = (q.blk + (N - 1 - n)) * (G::NF * 64) + lane;
 #pragma unroll
-        for (int s = 0; s < S64; ++s) {
-            const auto b = column_frag(dO, kGdrCols, s, kg, 16 * cg, r);
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (s >= G::first(t)) {
-                    X[t] = gd_mma<T>(tri.f[G::up(t, s)], b, X[t]);
-                    if constexpr (PRECISE) X[t] = gd_mma<T>(tri_lo.f[G::up(t, s)], b, X[t]);
+                for (int s = 0; s < S64; ++s)
+                    if (s >= G::first(T0 + t)) {
+                        x.p[t][s] = static_cast<const Frag *>(a.PT)[at + G::up(T0 + t, s) * 64];
+                        if constexpr (PRECISE) x.lo[t][s] = static_cast<const Frag *>(a.PT_lo)[at + G::up(T0 + t, s) * 64];
+                    }
+        };
+        auto ahead = [&](Set &x, int n) { // X, Y of step n
+            const T *qt = s_q[slot], *dO = s_do[slot];
+            const float *c = s_c[slot_c] + G::row(0, 4 * kg);
+            const int rows = n == 0 ? last + 1 : 64;
+            f32x4 X[NCG][2];
+            Frags<T, 4, PRECISE> Vb[NCG];
+#pragma unroll
+            for (int g = 0; g < NCG; ++g) {
+                zero_acc(X[g]);
+#pragma unroll
+                for (int s = 0; s < S64; ++s) {
+                    if (s < G::first(T0)) continue;
+                    const Frag b = column_frag(dO, COLS, s, kg, 16 * g, r);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        if (s >= G::first(T0 + t)) {
+                            X[g][t] = gd_mma<T>(x.p[t][s], b, X[g][t]);
+                            if constexpr (PRECISE) X[g][t] = gd_mma<T>(x.lo[t][s], b, X[g][t]);
+                        }
                 }
-        }
-        if (RING && n + 1 < N) get_tri(n + 1);
-        f32x4 V[4];
+            }
+            fetch(x, n + SETS);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            X[t] *= d.scale;
-            const int i0 = G::row(t, 4 * kg);
-            V[t] = widen4(column4(dO, kGdrCols, i0, 16 * cg, r)) * (*reinterpret_cast<const f32x4 *>(c + i0) * d.scale);
+            for (int g = 0; g < NCG; ++g) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) V[t][x] = i0 + x < rows ? V[t][x] : 0.f; // (what lies behind the last row is not zero)
-        }
-        Frags<T, 4, PRECISE> Vb;
-        Vb.from(V);
-        zero_acc(Y);
+                for (int t = 0; t < 2; ++t) s_x[g][T0 + t][lane] = X[g][t] * d.scale;
+                f32x4 V[4];
 #pragma unroll
-        for (int s = 0; s < S64; ++s)
+                for (int t = 0; t < 4; ++t) {
+                    V[t] = widen4(column4(dO + G::row(t, 0) * COLS, COLS, G::row(0, 4 * kg), 16 * g, r)) *
+                           (*reinterpret_cast<const f32x4 *>(c + G::row(t, 0)) * d.scale);
+                    if (rows < 64) { // (what lies behind the last row is not zero)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) Y[t] = Vb.mma(Tile::col_frag(qt, t, s, r, kg), s, Y[t]);
-    };
-    auto hand_over = [&] {
+                        for (int i = 0; i < 4; ++i) V[t][i] = G::row(t, 4 * kg) + i < rows ? V[t][i] : 0.f;
+                    }
+                }
+                Vb[g].from(V);
+            }
+            f32x4 Y[NCG][HT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) s_x[cg][t][lane] = X[t];
+            for (int g = 0; g < NCG; ++g) zero_acc(Y[g]);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) s_y[cg][t][lane] = Y[t];
-    };
-    __syncthreads();
-    ahead(0);
-    hand_over();
-    __syncthreads();
-    for (int n = 0; n <= N; ++n) {
+            for (int s = 0; s < S64; ++s)
+#pragma unroll
+                for (int t = 0; t < HT; ++t) {
+                    const Frag f = tile.col_frag(qt, T0 / 2 * HT + t, s);
+#pragma unroll
+                    for (int g = 0; g < NCG; ++g) Y[g][t] = Vb[g].mma(f, s, Y[g][t]);
+                }
+#pragma unroll
+            for (int g = 0; g < NCG; ++g)
+#pragma unroll
+                for (int t = 0; t < HT; ++t) s_y[g][T0 / 2 * HT + t][lane] = Y[g][t];
+            slot = next_slot<DQ>(slot);
+            slot_c = next_slot<DC>(slot_c);
+        };
+        auto store = [&](int m, int rows) { // dV, D of chunk m
+            const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0, reach = ((size_t)(rows - 1) * rsv + COLS) * sizeof(T);
+            store_tokens<T, NCG, SlateE::LD>(out_rows(static_cast<T *>(a.dv) + at, reach), rsv * (unsigned)sizeof(T), s_r, 32 * w, 32 * w, r, kg);
+            store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.dstates) + (q.blk + m) * DK * d.dv, (size_t)DK * d.dv * sizeof(T)), s_s, w, col0, lane);
+        };
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) fetch(sets[i], i);
+        all_arrived();
         __syncthreads();
-        if (n + 1 < N) ahead(n + 1);
+        ahead(sets[0], 0);
         __syncthreads();
-        if (n + 1 < N) hand_over();
-        if (n >= 1) {
-            const int m = N - n, rows = n == 1 ? last + 1 : 64; // chunk of step n - 1
-            store_tokens(static_cast<T *>(a.dv) + (q.v + (size_t)m * 64 * d.H) * d.dv + col, rsv, s_r[(n - 1) & 1][cg], rows, r, kg);
-            store_state<T, DK>(static_cast<T *>(a.dstates) + (q.blk + m) * DK * d.dv, s_s[(n - 1) & 1][cg], cg, col0, lane);
-        }
+        auto turn = [&](Set &x, int n) {
+            __syncthreads();
+            store(N - n, n == 1 ? last + 1 : 64);
+            __syncthreads();
+            ahead(x, n + 1);
+            if constexpr (!RING) __syncthreads();
+        };
+        // step 0
+        __syncthreads();
+        __syncthreads();
+        if (N > 1) ahead(sets[SETS - 1], 1);
         if constexpr (!RING) __syncthreads();
-    }
+        // steps 1 .. N - 2, whole turns without a branch inside (see out_rows): X, Y of steps 2 .. N - 1
+        int n = 1;
+        for (; n + SETS <= N - 1; n += SETS)
+#pragma unroll
+            for (int i = 0; i < SETS; ++i) turn(sets[i], n + i);
+        if (n <= N - 2) turn(sets[0], n++);
+        // the last two steps: nothing is ahead of them
+        for (; n <= N; ++n) {
+            __syncthreads();
+            store(N - n, n == 1 ? last + 1 : 64);
+            __syncthreads();
+            if constexpr (!RING) __syncthreads();
+        }
+    };
+    if (w == 0) beside(std::integral_constant<int, 0>{});
+    else beside(std::integral_constant<int, 2>{});
 }
 
-template <typename T, int DK, bool PRECISE> hipError_t launch(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {
-    return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / kGdrCols), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, PRECISE>), grid, dim3(kGdrThreads), 0, s, d, a, first);
+template <typename T, int DK, int NCG, bool PRECISE> hipError_t launch_cols(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {
+    return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
+        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, NCG, PRECISE>), grid, dim3((NCG + 4) * 64), 0, s, d, a, first);
     });
+}
+template <typename T, int DK, bool PRECISE> hipError_t launch(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {
+    return gdr_one_group(d) ? launch_cols<T, DK, 1, PRECISE>(d, a, s) : launch_cols<T, DK, 2, PRECISE>(d, a, s);
 }
 
 } // namespace

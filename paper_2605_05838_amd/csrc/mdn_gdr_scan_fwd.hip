@@ -2,8 +2,8 @@
 //     chain (waves 2, 3):   E = T (V - e^G K S),   S <- e^{G_C} S + K^T (e^{G_C - G} beta E)
 //     beside it, one chunk behind (waves 0, 1):   O = scale (e^G Q S + P E); stores of O, E and S
 // S and E reach the waves beside the chain through LDS, rounded to the storage type.
-// Bounds: a chunk's tiles are read by dv / 32 workgroups, of one XCD: 48 KB a step and CU at d = 128, which out of HBM and L2 arrive at
-// 37 B a clock and CU (1 320 clocks); the chain has 38 products of 16x16x32 (PRECISE 82) of 16 clocks on its SIMD.
+// Bounds: HBM where all CUs have a workgroup.  Below, the CU's loads: 16 KB each of K and Q, 6 of T and P, 1 KB of V per 8 columns a step,
+// of which a CU takes 25 to 37 B a clock.
 // PRECISE (a call that asks for the final states, which are 32-bit): S, T, V - e^G K S and e^{G_C - G} beta E enter their products as value +
 // remainder (K is exact in 16 bits), so that a state carries errors of 2^-17 and not of 2^-9.
 #include "mdn_gdr_scan.h"
@@ -12,73 +12,73 @@ namespace mdn {
 
 namespace {
 
-// REBUILD: E is given (in v's place), only the states are wanted
-template <typename T, int DK, bool PRECISE, bool REBUILD>
-__global__ __launch_bounds__(kGdrThreads) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
+// REBUILD: E is given (in v's place), only the states are wanted.  KEEP: E or the states are.
+template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP>
+__global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
     typedef Gd<T> G;
-    typedef GTile<T, DK> Tile;
+    typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
     typedef Slate<T, 64> SlateE;
-    constexpr int NT = DK / 16, SK = DK / G::KS, S64 = 64 / G::KS;
+    constexpr int NT = DK / 16, SK = DK / G::KS, S64 = 64 / G::KS, COLS = 16 * NCG, TRI = G::NF * 64 * G::E;
+    constexpr int TB = TRI * (int)sizeof(T);  // bytes of a triangle
+    constexpr int LDO = 32 + G::E;            // row length of what a wave beside the chain stores: 32 tokens of all columns, whole rows
     constexpr int D = sizeof(T) == 2 ? 3 : 1; // ring depth; 1: loads between two barriers, not beside the products
     constexpr int DC = D + 1;                 // of the coefficients, which both kinds of waves read
+    constexpr int SETS = sizeof(T) == 2 ? 2 : 1; // chunks of q and P that a wave beside the chain has asked for
     typedef GLoad<T, DK, true> LoadK;
-    typedef GLoad<T, kGdrCols, false> LoadV;
-    __shared__ __align__(16) T s_k[D][64 * DK], s_q[D][REBUILD ? 8 : 64 * DK], s_v[D][64 * kGdrCols];
+    typedef GLoad<T, COLS, false> LoadV;
+    __shared__ __align__(16) T s_k[D][64 * DK], s_v[D][64 * COLS], s_t[D][REBUILD ? 8 : TRI], s_tl[D][PRECISE ? TRI : 8];
     __shared__ __align__(16) float s_c[DC][kGdrCoef];
-    __shared__ __align__(16) T s_s[2][2][SlateS::SIZE], s_e[2][2][REBUILD ? 8 : SlateE::SIZE], s_o[2][REBUILD ? 8 : SlateE::SIZE];
+    __shared__ __align__(16) T s_s[2][NCG][SlateS::SIZE], s_e[2][REBUILD ? 8 : NCG * SlateE::SIZE], s_o[2][REBUILD ? 8 : COLS * LDO];
 
     const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, kg = lane >> 4;
     int bh, sub;
-    xcd_map(first + (int)blockIdx.x, d.dv / kGdrCols, bh, sub);
+    xcd_map(first + (int)blockIdx.x, d.dv / COLS, bh, sub);
     if (bh >= d.B * d.H) return;
     const GdrSeq q = gdr_seq(d, bh);
-    const int col0 = sub * kGdrCols, N = q.n, last = (q.len - 1) & 63; // last: the last row of the last chunk
+    const int col0 = sub * COLS, N = q.n, last = (q.len - 1) & 63; // last: the last row of the last chunk
     const unsigned rsv = (unsigned)(d.H * d.dv), rsk = (unsigned)(d.Hk * DK);
 
     // Step n: chunk n on the chain, chunk n - 1 beside it
-    if (w >= 4) { // ---- loads
-        const int w2 = w - 4;
+    if (w >= 2 + NCG) { // ---- loads
+        const int w2 = w - 2 - NCG;
         LoadK lk, lk_end;
         LoadV lv, lv_end;
-        const T *k = static_cast<const T *>(a.k) + q.k * DK, *qq = static_cast<const T *>(a.q) + q.k * DK;
-        const T *v = static_cast<const T *>(a.v) + q.v * d.dv + col0;
+        const T *k = static_cast<const T *>(a.k) + q.k * DK, *v = static_cast<const T *>(a.v) + q.v * d.dv + col0;
         lk.aim(rsk, w2, lane, 63);
         lv.aim(rsv, w2, lane, 63);
         lk_end.aim(rsk, w2, lane, last);
         lv_end.aim(rsv, w2, lane, last);
-        auto get_kv = [&](int n) {
+        auto request = [&](int n) {
+            if (w2 == 0) dma16(a.coef + (q.blk + n) * kGdrCoef, lane * 16, lds_addr(s_c[n % DC]));
             (n == N - 1 ? lk_end : lk).request(k + (size_t)n * 64 * rsk, s_k[n % D], w2);
             (n == N - 1 ? lv_end : lv).request(v + (size_t)n * 64 * rsv, s_v[n % D], w2);
-            if (w2 == 0) dma16(a.coef + (q.blk + n) * kGdrCoef, lane * 16, lds_addr(s_c[n % DC]));
-        };
-        auto get_q = [&](int n) {
-            if constexpr (!REBUILD) (n == N - 1 ? lk_end : lk).request(qq + (size_t)n * 64 * rsk, s_q[n % D], w2);
+            if constexpr (!REBUILD) load_block<TB>(a.T, q.blk + n, s_t[n % D], w2, lane);
+            if constexpr (PRECISE) load_block<TB>(a.T_lo, q.blk + n, s_tl[n % D], w2, lane);
         };
         if constexpr (D == 1) {
             for (int n = 0; n <= N; ++n) {
-                if (n >= 1) get_q(n - 1);
-                if (n < N) get_kv(n);
+                if (n < N) request(n);
                 wait_vm<0>();
                 __syncthreads();
                 __syncthreads();
             }
         } else {
-            constexpr int KV = LoadK::COUNT + LoadV::COUNT, STEP = KV + (REBUILD ? 0 : LoadK::COUNT);
-            get_kv(0);
-            get_q(0);
+            // requests of a chunk by either wave (the first one's coefficients included)
+            constexpr int C1 = LoadK::COUNT + LoadV::COUNT + (REBUILD ? 0 : TB / 2048) + (PRECISE ? TB / 2048 : 0), C0 = C1 + 1;
+            auto all_but_last = [&] { w2 == 0 ? wait_vm<C0>() : wait_vm<C1>(); };
+            request(0);
             if (N > 1) {
-                get_kv(1);
-                w2 == 0 ? wait_vm<KV + 1>() : wait_vm<KV>();
+                request(1);
+                all_but_last();
             } else {
                 wait_vm<0>();
             }
             for (int n = 0; n <= N; ++n) {
                 __syncthreads();
-                if (n + 1 < N) get_q(n + 1); // (for step n + 2)
                 if (n + 2 < N) {
-                    get_kv(n + 2);
-                    w2 == 0 ? wait_vm<STEP + 1>() : wait_vm<STEP>();
+                    request(n + 2);
+                    all_but_last();
                 } else {
                     wait_vm<0>();
                 }
@@ -87,21 +87,28 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_fwd_kernel(GdrDims d, Gd
         return;
     }
 
-    const int cg = w & 1, col = col0 + 16 * cg;
+    const TileReader<T, DK> tile(r, kg);
     if (w >= 2) { // ---- the chain
-        Triangle<T> tri;
-        TriangleIf<T, PRECISE> tri_lo;
-        if constexpr (!REBUILD) {
-            tri.load(a.T, q.blk, lane);
-            tri_lo.load(a.T_lo, q.blk, lane);
-        }
+        const int cg = w - 2, col = col0 + 16 * cg;
+        int slot = 0, slot_c = 0;
         f32x4 S[NT];
         load_state<T>(S, a.S0 ? a.S0 + q.state * DK * d.dv : nullptr, d.dv, col, r, kg);
+        all_arrived();
         for (int n = 0; n <= N; ++n) {
             __syncthreads();
             if (n < N) {
-                const T *k = s_k[n % D], *v = s_v[n % D];
-                const float *c = s_c[n % DC];
+                const T *k = s_k[slot], *v = s_v[slot], *tri = s_t[slot], *tri_lo = s_tl[slot];
+                const float *c = s_c[slot_c] + G::row(0, 4 * kg);
+                // what the chain has to wait for least: V, the decays
+                decltype(column4(v, 0, 0, 0, 0)) V[4];
+                f32x4 eg[4], ec[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    V[t] = column4(v + G::row(t, 0) * COLS, COLS, G::row(0, 4 * kg), 16 * cg, r);
+                    if constexpr (!REBUILD) eg[t] = *reinterpret_cast<const f32x4 *>(c + G::row(t, 0));
+                    ec[t] = *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 0));
+                }
+                const float eC = s_c[slot_c][63];
                 Frags<T, NT, PRECISE> Sb;
                 Sb.from(S);
 #pragma unroll
@@ -109,19 +116,16 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_fwd_kernel(GdrDims d, Gd
                 f32x4 E[4];
                 if constexpr (REBUILD) {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) E[t] = widen4(column4(v, kGdrCols, G::row(t, 4 * kg), 16 * cg, r));
+                    for (int t = 0; t < 4; ++t) E[t] = widen4(V[t]);
                 } else {
                     f32x4 R[4];
                     zero_acc(R);
 #pragma unroll
                     for (int s = 0; s < SK; ++s)
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) R[t] = Sb.mma(Tile::row_frag(k, G::row(t, r), s, kg), s, R[t]);
+                        for (int t = 0; t < 4; ++t) R[t] = Sb.mma(tile.row_frag(k, t, s), s, R[t]);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const f32x4 eg = *reinterpret_cast<const f32x4 *>(c + G::row(t, 4 * kg));
-                        R[t] = widen4(column4(v, kGdrCols, G::row(t, 4 * kg), 16 * cg, r)) - eg * R[t];
-                    }
+                    for (int t = 0; t < 4; ++t) R[t] = widen4(V[t]) - eg[t] * R[t];
                     Frags<T, 4, PRECISE> Rb;
                     Rb.from(R);
                     zero_acc(E);
@@ -130,19 +134,14 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_fwd_kernel(GdrDims d, Gd
 #pragma unroll
                         for (int t = 0; t < 4; ++t)
                             if (s <= G::last(t)) {
-                                E[t] = Rb.mma(tri.f[G::low(t, s)], s, E[t]);
-                                if constexpr (PRECISE) E[t] = gd_mma<T>(tri_lo.f[G::low(t, s)], Rb.hi[s], E[t]);
+                                E[t] = Rb.mma(tri_frag(tri, G::low(t, s), lane), s, E[t]);
+                                if constexpr (PRECISE) E[t] = gd_mma<T>(tri_frag(tri_lo, G::low(t, s), lane), Rb.hi[s], E[t]);
                             }
-                    if (n + 1 < N) {
-                        tri.load(a.T, q.blk + n + 1, lane);
-                        tri_lo.load(a.T_lo, q.blk + n + 1, lane);
-                    }
 #pragma unroll
-                    for (int s = 0; s < S64; ++s) SlateE::put(s_e[n & 1][cg], s, r, kg, G::frag(&E[s * G::KT]));
+                    for (int s = 0; s < S64; ++s) SlateE::put(s_e[n & 1] + cg * SlateE::SIZE, s, r, kg, G::frag(&E[s * G::KT]));
                 }
-                const float eC = c[63];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) E[t] *= *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 4 * kg));
+                for (int t = 0; t < 4; ++t) E[t] *= ec[t];
                 Frags<T, 4, PRECISE> Eb;
                 Eb.from(E);
 #pragma unroll
@@ -150,7 +149,9 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_fwd_kernel(GdrDims d, Gd
 #pragma unroll
                 for (int s = 0; s < S64; ++s)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) S[t] = Eb.mma(Tile::col_frag(k, t, s, r, kg), s, S[t]);
+                    for (int t = 0; t < NT; ++t) S[t] = Eb.mma(tile.col_frag(k, t, s), s, S[t]);
+                slot = next_slot<D>(slot);
+                slot_c = next_slot<DC>(slot_c);
             }
             if constexpr (D == 1) __syncthreads();
         }
@@ -158,53 +159,116 @@ __global__ __launch_bounds__(kGdrThreads) void gdr_scan_fwd_kernel(GdrDims d, Gd
         return;
     }
 
-    // ---- beside the chain
-    Triangle<T> tri;
-    if constexpr (!REBUILD) tri.load(a.P, q.blk, lane);
-    for (int n = 0; n <= N; ++n) {
-        __syncthreads();
-        if (n >= 1) {
-            const int m = n - 1, rows = m == N - 1 ? last + 1 : 64;
-            const T *ss = s_s[m & 1][cg];
-            if constexpr (!REBUILD) {
-                const T *qt = s_q[m % D], *se = s_e[m & 1][cg];
-                const float *c = s_c[m % DC];
-                f32x4 O[4];
-                zero_acc(O);
+    // ---- beside the chain: 32 tokens of a chunk, all columns.  Its q rows and fragments of P are nobody else's and come straight into
+    // registers, SETS chunks ahead.
+    auto beside = [&](auto first_tile) {
+        constexpr int T0 = decltype(first_tile)::value;
+        struct Set { Frag q[2][SK], p[2][S64]; } sets[SETS];
+        int slot_c = 0;
+        unsigned qo[2], qo_end[2];
 #pragma unroll
-                for (int s = 0; s < SK; ++s) {
-                    const auto b = SlateS::get(ss, s, r, kg);
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) O[t] = gd_mma<T>(Tile::row_frag(qt, G::row(t, r), s, kg), b, O[t]);
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) O[t] *= *reinterpret_cast<const f32x4 *>(c + G::row(t, 4 * kg));
-#pragma unroll
-                for (int s = 0; s < S64; ++s) {
-                    const auto b = SlateE::get(se, s, r, kg);
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        if (s <= G::last(t)) O[t] = gd_mma<T>(tri.f[G::low(t, s)], b, O[t]);
-                }
-                if (n < N) tri.load(a.P, q.blk + n, lane);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) O[t] *= d.scale;
-#pragma unroll
-                for (int s = 0; s < S64; ++s) SlateE::put(s_o[cg], s, r, kg, G::frag(&O[s * G::KT]));
-                const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col;
-                store_tokens(static_cast<T *>(a.o) + at, rsv, s_o[cg], rows, r, kg);
-                if (a.e) store_tokens(static_cast<T *>(a.e) + at, rsv, se, rows, r, kg);
-            }
-            if (a.states) store_state<T, DK>(static_cast<T *>(a.states) + (q.blk + m) * DK * d.dv, ss, cg, col0, lane);
+        for (int t = 0; t < 2; ++t) {
+            const int row = G::row(T0 + t, r);
+            qo[t] = (unsigned)row * rsk + kg * G::E;
+            qo_end[t] = (unsigned)min(row, last) * rsk + kg * G::E;
         }
+        auto fetch = [&](Set &x, int m) {
+            m = min(m, N - 1); // (asked for again behind the last chunk: no branch around loads in flight)
+            const T *qq = static_cast<const T *>(a.q) + q.k * DK + (size_t)m * 64 * rsk;
+            const Frag *p = static_cast<const Frag *>(a.P) + (q.blk + m) * (G::NF * 64) + lane;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const T *row = at32(qq, m == N - 1 ? qo_end[t] : qo[t]);
+#pragma unroll
+                for (int s = 0; s < SK; ++s) x.q[t][s] = *reinterpret_cast<const Frag *>(row + s * G::KS);
+#pragma unroll
+                for (int s = 0; s < S64; ++s)
+                    if (s <= G::last(T0 + t)) x.p[t][s] = p[G::low(T0 + t, s) * 64];
+            }
+        };
+        auto step = [&](Set &x, int m) {
+            const int rows = m == N - 1 ? last + 1 : 64;
+            if constexpr (!REBUILD) {
+                const T *se = s_e[m & 1];
+                const float *c = s_c[slot_c] + G::row(0, 4 * kg);
+                f32x4 O[NCG][2];
+#pragma unroll
+                for (int g = 0; g < NCG; ++g) zero_acc(O[g]);
+#pragma unroll
+                for (int s = 0; s < SK; ++s)
+#pragma unroll
+                    for (int g = 0; g < NCG; ++g) {
+                        const Frag b = SlateS::get(s_s[m & 1][g], s, r, kg);
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) O[g][t] = gd_mma<T>(x.q[t][s], b, O[g][t]);
+                    }
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int g = 0; g < NCG; ++g) O[g][t] *= *reinterpret_cast<const f32x4 *>(c + G::row(T0 + t, 0));
+#pragma unroll
+                for (int s = 0; s < S64; ++s)
+#pragma unroll
+                    for (int g = 0; g < NCG; ++g) {
+                        if (s > G::last(T0 + 1)) continue;
+                        const Frag b = SlateE::get(se + g * SlateE::SIZE, s, r, kg);
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            if (s <= G::last(T0 + t)) O[g][t] = gd_mma<T>(x.p[t][s], b, O[g][t]);
+                    }
+                fetch(x, m + SETS);
+#pragma unroll
+                for (int g = 0; g < NCG; ++g) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) O[g][t] *= d.scale;
+#pragma unroll
+                    for (int s = 0; s < 2 / G::KT; ++s)
+                        *reinterpret_cast<Frag *>(s_o[w] + (16 * g + r) * LDO + s * G::KS + kg * G::E) = G::frag(&O[g][s * G::KT]);
+                }
+                const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0, reach = ((size_t)(rows - 1) * rsv + COLS) * sizeof(T);
+                store_tokens<T, NCG, LDO>(out_rows(static_cast<T *>(a.o) + at, reach), rsv * (unsigned)sizeof(T), s_o[w], 0, 32 * w, r, kg);
+                if constexpr (KEEP)
+                    store_tokens<T, NCG, SlateE::LD>(out_rows(static_cast<T *>(a.e) + at, a.e ? reach : 0), rsv * (unsigned)sizeof(T), se, 32 * w,
+                                                     32 * w, r, kg);
+                slot_c = next_slot<DC>(slot_c);
+            }
+            if constexpr (KEEP)
+                store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.states) + (q.blk + m) * DK * d.dv, a.states ? (size_t)DK * d.dv * sizeof(T) : 0),
+                                        s_s[m & 1], w, col0, lane);
+        };
+        if constexpr (!REBUILD) {
+#pragma unroll
+            for (int i = 0; i < SETS; ++i) fetch(sets[i], i);
+            all_arrived();
+        }
+        __syncthreads();
         if constexpr (D == 1) __syncthreads();
-    }
+        auto turn = [&](Set &x, int m) {
+            __syncthreads();
+            step(x, m);
+            if constexpr (D == 1) __syncthreads();
+        };
+        int m = 0;
+        for (; m + SETS <= N; m += SETS) // (whole turns, without a branch inside: see out_rows)
+#pragma unroll
+            for (int i = 0; i < SETS; ++i) turn(sets[i], m + i);
+        if (m < N) turn(sets[0], m);
+    };
+    if (w == 0) beside(std::integral_constant<int, 0>{});
+    else beside(std::integral_constant<int, 2>{});
 }
 
-template <typename T, int DK, bool PRECISE, bool REBUILD> hipError_t launch(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
-    return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / kGdrCols), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, PRECISE, REBUILD>), grid, dim3(kGdrThreads), 0, s, d, a, first);
+template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP> hipError_t launch_keep(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
+    return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
+        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, NCG, PRECISE, REBUILD, KEEP>), grid, dim3((NCG + 4) * 64), 0, s, d, a, first);
     });
+}
+template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD> hipError_t launch_cols(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
+    if (REBUILD || a.e || a.states) return launch_keep<T, DK, NCG, PRECISE, REBUILD, true>(d, a, s);
+    return launch_keep<T, DK, NCG, PRECISE, REBUILD, REBUILD>(d, a, s);
+}
+template <typename T, int DK, bool PRECISE, bool REBUILD> hipError_t launch(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
+    return gdr_one_group(d) ? launch_cols<T, DK, 1, PRECISE, REBUILD>(d, a, s) : launch_cols<T, DK, 2, PRECISE, REBUILD>(d, a, s);
 }
 
 } // namespace
