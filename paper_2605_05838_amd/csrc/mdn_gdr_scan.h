@@ -1,15 +1,17 @@
 // What the forward and the reverse scan of the gated delta rule have in common.
 //
 // A workgroup walks the chunks of one (sequence, value head) pair for NCG groups of 16 columns of the state, one step per chunk, with
-// three kinds of waves (in this order: dealt to the four SIMDs in turn, the chain shares its own with the loads at most):
-//   2 waves     beside the chain: what hangs on it without being part of it, and every store;
-//   NCG waves   the chain: 16 columns each, the state in their accumulators (see mdn_gdr.h);
-//   2 waves     loads: the chunks ahead, HBM -> LDS without registers, into rings.
-// The chain itself takes 640 clocks a step at d = 128, the products' time; everything else must stay out of its way.  So it loads nothing: the
-// fragments of T, asked for by the wave that wants them as soon as those of the chunk before were used up, came back 2 000 clocks later, behind
-// all of the step's tiles, and were what a step waited for (2 050 clocks, and 4 100 with the remainders of T).  A chunk's tiles take 1 300 clocks
-// and more from the request to the last line, so that two chunks are on their way while one is worked on: rings of three (of two: 2 350 clocks a
-// step where three take 1 340).
+// three kinds of waves:
+//   2 waves       beside the chain: what hangs on it without being part of it, and every store;
+//   NCG waves     the chain: the state in their accumulators (see mdn_gdr.h); in fp32 and with remainders, forward, two waves to 16 columns;
+//   2 waves       loads: the chunks ahead, HBM -> LDS without registers, into rings.
+// A chain wave is bound by its LDS instructions, ~26 clocks each, most of them reads of A operands: 2 050 clocks a step at d = 128 in 16
+// bits, 3 650 with remainders.  Two waves to 16 columns each form the products of half of the tokens with the whole state, whose other half
+// they find in LDS since the step's barrier, hand them to the other one, and then have all they need for half of the next state; the small
+// products with T in between both form.
+// The chain loads nothing: the fragments of T, asked for by the wave that wants them as soon as those of the chunk before were used up, came
+// back 2 000 clocks later, behind all of the step's tiles.  A chunk's tiles take 1 300 clocks and more from the request to the last line, so that two chunks
+// are on their way while one is worked on: rings of three (of two: 2 350 clocks a step where three take 1 340).
 #pragma once
 #include "mdn_gdr.h"
 
@@ -146,18 +148,30 @@ __device__ __forceinline__ void store_state(__amdgpu_buffer_rsrc_t block, const 
     }
 }
 
-// a wave's state tiles from and to a [dk][dv] fp32 tensor, column col + r
-template <typename T, int NT> __device__ __forceinline__ void load_state(f32x4 (&S)[NT], const float *g, int dv, int col, int r, int kg) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) S[t][x] = g ? g[(size_t)(Gd<T>::row(t, 4 * kg) + x) * dv + col + r] : 0.f;
+// Two waves of the same 16 columns wait for each other: `mine` says that this one's fragments of step n are in LDS (a wave's LDS operations are
+// done in order), and it goes on when the other one's are.  Both are waves of one workgroup: the wait ends.
+__device__ __forceinline__ void say(int *mine, int n) {
+    asm volatile("" : : : "memory");
+    *const_cast<volatile int *>(mine) = n + 1;
+    asm volatile("" : : : "memory");
 }
-template <typename T, int NT> __device__ __forceinline__ void save_state(const f32x4 (&S)[NT], float *g, int dv, int col, int r, int kg) {
+__device__ __forceinline__ void wait_for(const int *other, int n) {
+    while (__builtin_amdgcn_readfirstlane(*const_cast<const volatile int *>(other)) <= n) {}
+    asm volatile("" : : : "memory");
+}
+
+// a wave's state tiles (from tile T0 on) from and to a [dk][dv] fp32 tensor, column col + r
+template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void load_state(f32x4 (&S)[NT], const float *g, int dv, int col, int r, int kg) {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) g[(size_t)(Gd<T>::row(t, 4 * kg) + x) * dv + col + r] = S[t][x];
+        for (int x = 0; x < 4; ++x) S[t][x] = g ? g[(size_t)(Gd<T>::row(T0 + t, 4 * kg) + x) * dv + col + r] : 0.f;
+}
+template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void save_state(const f32x4 (&S)[NT], float *g, int dv, int col, int r, int kg) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) g[(size_t)(Gd<T>::row(T0 + t, 4 * kg) + x) * dv + col + r] = S[t][x];
 }
 
 // 16 columns per workgroup while the CUs hold all of those workgroups, or 32

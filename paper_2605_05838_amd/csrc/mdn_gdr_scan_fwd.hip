@@ -1,6 +1,6 @@
 // Gated delta rule, forward scan and reconstruction of the chunk-start states.  Per chunk, S the state at its start:
-//     chain (waves 2, 3):   E = T (V - e^G K S),   S <- e^{G_C} S + K^T (e^{G_C - G} beta E)
-//     beside it, one chunk behind (waves 0, 1):   O = scale (e^G Q S + P E); stores of O, E and S
+//     chain:   E = T (V - e^G K S),   S <- e^{G_C} S + K^T (e^{G_C - G} beta E)
+//     beside it, one chunk behind:   O = scale (e^G Q S + P E); stores of O, E and S
 // S and E reach the waves beside the chain through LDS, rounded to the storage type.
 // Bounds: HBM where all CUs have a workgroup.  Below, the CU's loads: 16 KB each of K and Q, 6 of T and P, 1 KB of V per 8 columns a step,
 // of which a CU takes 25 to 37 B a clock.
@@ -12,14 +12,20 @@ namespace mdn {
 
 namespace {
 
+// Waves to 16 columns of the chain.  Two share the products, and pay for it by what they hand to each other and wait for: 48 us for 65 in
+// fp32 ([2, 1 024] tokens, 4 heads, d = 64), 27 for 30 with remainders (777 tokens, 16 heads, d = 128), but 146 for 133 in 16 bits
+// ([4, 4 096] tokens, 16 heads, d = 128), where one wave's products are done before the chunk behind them is there.
+template <typename T, int NCG, bool PRECISE> constexpr int CW = sizeof(T) == 4 || (PRECISE && NCG == 1) ? 2 : 1;
+
 // REBUILD: E is given (in v's place), only the states are wanted.  KEEP: E or the states are.
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP>
-__global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
+__global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
     typedef Gd<T> G;
     typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
     typedef Slate<T, 64> SlateE;
     constexpr int NT = DK / 16, SK = DK / G::KS, S64 = 64 / G::KS, COLS = 16 * NCG, TRI = G::NF * 64 * G::E;
+    constexpr int CWS = CW<T, NCG, PRECISE>, NS = CWS + 1; // NS: slots of S
     constexpr int TB = TRI * (int)sizeof(T);  // bytes of a triangle
     constexpr int LDO = 32 + G::E;            // row length of what a wave beside the chain stores: 32 tokens of all columns, whole rows
     constexpr int D = sizeof(T) == 2 ? 3 : 1; // ring depth; 1: loads between two barriers, not beside the products
@@ -29,7 +35,11 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d,
     typedef GLoad<T, COLS, false> LoadV;
     __shared__ __align__(16) T s_k[D][64 * DK], s_v[D][64 * COLS], s_t[D][REBUILD ? 8 : TRI], s_tl[D][PRECISE ? TRI : 8];
     __shared__ __align__(16) float s_c[DC][kGdrCoef];
-    __shared__ __align__(16) T s_s[2][NCG][SlateS::SIZE], s_e[2][REBUILD ? 8 : NCG * SlateE::SIZE], s_o[2][REBUILD ? 8 : COLS * LDO];
+    // S: with two waves, read by the other one when it is new, beside the chain a step later, and written for the step after that meanwhile
+    __shared__ __align__(16) T s_s[NS][NCG][SlateS::SIZE], s_sl[NCG][CWS == 2 && PRECISE ? SlateS::SIZE : 8];
+    __shared__ __align__(16) Frag s_x[NCG][CWS == 2 ? S64 : 1][64], s_xl[NCG][CWS == 2 && PRECISE ? S64 : 1][64]; // V - e^G K S, from wave to wave
+    __shared__ int s_said[NCG][2]; // steps whose half of it is there
+    __shared__ __align__(16) T s_e[2][REBUILD ? 8 : NCG * SlateE::SIZE], s_o[2][REBUILD ? 8 : COLS * LDO];
 
     const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, kg = lane >> 4;
     int bh, sub;
@@ -40,8 +50,8 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d,
     const unsigned rsv = (unsigned)(d.H * d.dv), rsk = (unsigned)(d.Hk * DK);
 
     // Step n: chunk n on the chain, chunk n - 1 beside it
-    if (w >= 2 + NCG) { // ---- loads
-        const int w2 = w - 2 - NCG;
+    if (w >= 2 + CWS * NCG) { // ---- loads
+        const int w2 = w - 2 - CWS * NCG;
         LoadK lk, lk_end;
         LoadV lv, lv_end;
         const T *k = static_cast<const T *>(a.k) + q.k * DK, *v = static_cast<const T *>(a.v) + q.v * d.dv + col0;
@@ -88,74 +98,127 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d,
     }
 
     const TileReader<T, DK> tile(r, kg);
-    if (w >= 2) { // ---- the chain
-        const int cg = w - 2, col = col0 + 16 * cg;
-        int slot = 0, slot_c = 0;
-        f32x4 S[NT];
-        load_state<T>(S, a.S0 ? a.S0 + q.state * DK * d.dv : nullptr, d.dv, col, r, kg);
+    auto chain = [&](auto half) {
+        // this wave's half (or all): of dk and of the tokens
+        constexpr int TW = decltype(half)::value, HT = NT / CWS, HS = SK / CWS, H64 = S64 / CWS, RT = 4 / CWS;
+        const int cg = (w - 2) / CWS, col = col0 + 16 * cg;
+        int slot = 0, slot_c = 0, slot_s = 0;
+        f32x4 S[HT];
+        Frags<T, HT, PRECISE> Sb;
+        load_state<T, TW * HT>(S, a.S0 ? a.S0 + q.state * DK * d.dv : nullptr, d.dv, col, r, kg);
         all_arrived();
+        auto publish = [&] { // S, for the waves beside the chain and the other half's
+#pragma unroll
+            for (int s = 0; s < HS; ++s) {
+                SlateS::put(s_s[slot_s][cg], TW * HS + s, r, kg, Sb.hi[s]);
+                if constexpr (PRECISE && CWS == 2) SlateS::put(s_sl[cg], TW * HS + s, r, kg, Sb.lo[s]);
+            }
+        };
+        Sb.from(S);
+        if constexpr (CWS == 2) publish();
+        if (lane == 0) s_said[cg][TW] = 0;
         for (int n = 0; n <= N; ++n) {
             __syncthreads();
             if (n < N) {
                 const T *k = s_k[slot], *v = s_v[slot], *tri = s_t[slot], *tri_lo = s_tl[slot];
                 const float *c = s_c[slot_c] + G::row(0, 4 * kg);
-                // what the chain has to wait for least: V, the decays
-                decltype(column4(v, 0, 0, 0, 0)) V[4];
-                f32x4 eg[4], ec[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    V[t] = column4(v + G::row(t, 0) * COLS, COLS, G::row(0, 4 * kg), 16 * cg, r);
-                    if constexpr (!REBUILD) eg[t] = *reinterpret_cast<const f32x4 *>(c + G::row(t, 0));
-                    ec[t] = *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 0));
-                }
                 const float eC = s_c[slot_c][63];
-                Frags<T, NT, PRECISE> Sb;
-                Sb.from(S);
-#pragma unroll
-                for (int s = 0; s < SK; ++s) SlateS::put(s_s[n & 1][cg], s, r, kg, Sb.hi[s]);
+                if constexpr (CWS == 1) publish();
                 f32x4 E[4];
                 if constexpr (REBUILD) {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) E[t] = widen4(V[t]);
+                    for (int t = 0; t < 4; ++t) E[t] = widen4(column4(v + G::row(t, 0) * COLS, COLS, G::row(0, 4 * kg), 16 * cg, r));
                 } else {
-                    f32x4 R[4];
+                    Frag other[HS], other_lo[PRECISE ? HS : 1];
+#pragma unroll
+                    for (int s = 0; s < (CWS - 1) * HS; ++s) {
+                        other[s] = SlateS::get(s_s[slot_s][cg], (1 - TW) * HS + s, r, kg);
+                        if constexpr (PRECISE) other_lo[s] = SlateS::get(s_sl[cg], (1 - TW) * HS + s, r, kg);
+                    }
+                    f32x4 R[RT];
                     zero_acc(R);
 #pragma unroll
-                    for (int s = 0; s < SK; ++s)
+                    for (int s = 0; s < HS; ++s)
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) R[t] = Sb.mma(tile.row_frag(k, t, s), s, R[t]);
+                        for (int t = 0; t < RT; ++t) R[t] = Sb.mma(tile.row_frag(k, RT * TW + t, TW * HS + s), s, R[t]);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) R[t] = widen4(V[t]) - eg[t] * R[t];
-                    Frags<T, 4, PRECISE> Rb;
+                    for (int s = 0; s < (CWS - 1) * HS; ++s)
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) {
+                            const Frag f = tile.row_frag(k, RT * TW + t, (1 - TW) * HS + s);
+                            R[t] = gd_mma<T>(f, other[s], R[t]);
+                            if constexpr (PRECISE) R[t] = gd_mma<T>(f, other_lo[s], R[t]);
+                        }
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        const int t0 = G::row(RT * TW + t, 0);
+                        R[t] = widen4(column4(v + t0 * COLS, COLS, G::row(0, 4 * kg), 16 * cg, r)) - *reinterpret_cast<const f32x4 *>(c + t0) * R[t];
+                    }
+                    Frags<T, RT, PRECISE> Rb;
                     Rb.from(R);
-                    zero_acc(E);
+                    if constexpr (CWS == 2) {
 #pragma unroll
-                    for (int s = 0; s < S64; ++s)
+                        for (int s = 0; s < H64; ++s) {
+                            s_x[cg][TW * H64 + s][lane] = Rb.hi[s];
+                            if constexpr (PRECISE) s_xl[cg][TW * H64 + s][lane] = Rb.lo[s];
+                        }
+                        say(&s_said[cg][TW], n);
+                    }
+                    // Own tokens first, while the other wave's are not there yet.  Sums over the first and over the second half of the tokens, so that both waves have the same bits
+                    f32x4 X[2];
+                    zero_acc(E);
+                    zero_acc(X);
+                    auto add = [&](int s, Frag hi, Frag lo) {
 #pragma unroll
                         for (int t = 0; t < 4; ++t)
                             if (s <= G::last(t)) {
-                                E[t] = Rb.mma(tri_frag(tri, G::low(t, s), lane), s, E[t]);
-                                if constexpr (PRECISE) E[t] = gd_mma<T>(tri_frag(tri_lo, G::low(t, s), lane), Rb.hi[s], E[t]);
+                                f32x4 &to = CWS == 1 || s < H64 ? E[t] : X[t & 1];
+                                const Frag f = tri_frag(tri, G::low(t, s), lane);
+                                to = gd_mma<T>(f, hi, to);
+                                if constexpr (PRECISE) {
+                                    to = gd_mma<T>(f, lo, to);
+                                    to = gd_mma<T>(tri_frag(tri_lo, G::low(t, s), lane), hi, to);
+                                }
                             }
+                    };
 #pragma unroll
-                    for (int s = 0; s < S64; ++s) SlateE::put(s_e[n & 1] + cg * SlateE::SIZE, s, r, kg, G::frag(&E[s * G::KT]));
+                    for (int s = 0; s < H64; ++s) add(TW * H64 + s, Rb.hi[s], Rb.lo[PRECISE ? s : 0]);
+                    if constexpr (CWS == 2) {
+                        wait_for(&s_said[cg][1 - TW], n);
+#pragma unroll
+                        for (int s = 0; s < H64; ++s) {
+                            const int so = (1 - TW) * H64 + s;
+                            add(so, s_x[cg][so][lane], s_xl[cg][PRECISE ? so : 0][lane]);
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) E[2 + t] += X[t];
+                    }
+#pragma unroll
+                    for (int s = TW * H64; s < (TW + 1) * H64; ++s) SlateE::put(s_e[n & 1] + cg * SlateE::SIZE, s, r, kg, G::frag(&E[s * G::KT]));
                 }
 #pragma unroll
-                for (int t = 0; t < 4; ++t) E[t] *= ec[t];
+                for (int t = 0; t < 4; ++t) E[t] *= *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 0));
                 Frags<T, 4, PRECISE> Eb;
                 Eb.from(E);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) S[t] *= eC;
+                for (int t = 0; t < HT; ++t) S[t] *= eC;
 #pragma unroll
                 for (int s = 0; s < S64; ++s)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) S[t] = Eb.mma(tile.col_frag(k, t, s), s, S[t]);
+                    for (int t = 0; t < HT; ++t) S[t] = Eb.mma(tile.col_frag(k, TW * HT + t, s), s, S[t]);
                 slot = next_slot<D>(slot);
                 slot_c = next_slot<DC>(slot_c);
+                slot_s = next_slot<NS>(slot_s);
+                Sb.from(S);
+                if constexpr (CWS == 2) publish();
             }
             if constexpr (D == 1) __syncthreads();
         }
-        if (a.S_final) save_state<T>(S, a.S_final + q.state * DK * d.dv, d.dv, col, r, kg);
+        if (a.S_final) save_state<T, TW * HT>(S, a.S_final + q.state * DK * d.dv, d.dv, col, r, kg);
+    };
+    if (w >= 2) { // ---- the chain
+        if (CWS == 1 || w % 2 == 0) chain(std::integral_constant<int, 0>{});
+        else chain(std::integral_constant<int, CWS - 1>{});
         return;
     }
 
@@ -186,6 +249,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d,
                     if (s <= G::last(T0 + t)) x.p[t][s] = p[G::low(T0 + t, s) * 64];
             }
         };
+        int slot_s = 0;
         auto step = [&](Set &x, int m) {
             const int rows = m == N - 1 ? last + 1 : 64;
             if constexpr (!REBUILD) {
@@ -198,7 +262,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d,
                 for (int s = 0; s < SK; ++s)
 #pragma unroll
                     for (int g = 0; g < NCG; ++g) {
-                        const Frag b = SlateS::get(s_s[m & 1][g], s, r, kg);
+                        const Frag b = SlateS::get(s_s[slot_s][g], s, r, kg);
 #pragma unroll
                         for (int t = 0; t < 2; ++t) O[g][t] = gd_mma<T>(x.q[t][s], b, O[g][t]);
                     }
@@ -234,7 +298,8 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d,
             }
             if constexpr (KEEP)
                 store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.states) + (q.blk + m) * DK * d.dv, a.states ? (size_t)DK * d.dv * sizeof(T) : 0),
-                                        s_s[m & 1], w, col0, lane);
+                                        s_s[slot_s], w, col0, lane);
+            slot_s = next_slot<NS>(slot_s);
         };
         if constexpr (!REBUILD) {
 #pragma unroll
@@ -260,7 +325,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d,
 
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP> hipError_t launch_keep(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
     return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, NCG, PRECISE, REBUILD, KEEP>), grid, dim3((NCG + 4) * 64), 0, s, d, a, first);
+        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, NCG, PRECISE, REBUILD, KEEP>), grid, dim3((CW<T, NCG, PRECISE> * NCG + 4) * 64), 0, s, d, a, first);
     });
 }
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD> hipError_t launch_cols(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
