@@ -45,6 +45,7 @@ struct GdrScanFwdArgs {
     const float *S0;
     void *o, *e, *states; // e, states may be null
     float *S_final;       // may be null
+    int touch;            // whether later chunks are brought into the L2; the launch sets it
 };
 struct GdrScanBwdArgs {
     const void *q, *k, *dO;

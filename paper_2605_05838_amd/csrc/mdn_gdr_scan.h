@@ -1,19 +1,21 @@
 // What the forward and the reverse scan of the gated delta rule have in common.
 //
 // A workgroup walks the chunks of one (sequence, value head) pair for NCG groups of 16 columns of the state, one step per chunk, with
-// three kinds of waves:
-//   2 waves       beside the chain: what hangs on it without being part of it, and every store;
+// four kinds of waves:
+//   2 waves       beside the chain: what hangs on it without being part of it;
 //   NCG waves     the chain: the state in their accumulators (see mdn_gdr.h); in fp32 and with remainders, forward, two waves to 16 columns;
-//   2 waves       loads: the chunks ahead, HBM -> LDS without registers, into rings.
+//   2 waves       loads: the chunks ahead, HBM -> LDS without registers, into rings;
+//   2 waves       stores, out of LDS, and lines for later (GdrTouch); in fp32 the loading waves, whose loads are not beside the products.
 // A chain wave is bound by its LDS instructions, ~26 clocks each, most of them reads of A operands: 2 050 clocks a step at d = 128 in 16
 // bits, 3 650 with remainders.  Two waves to 16 columns each form the products of half of the tokens with the whole state, whose other half
 // they find in LDS since the step's barrier, hand them to the other one, and then have all they need for half of the next state; the small
 // products with T in between both form.
 // The chain loads nothing: the fragments of T, asked for by the wave that wants them as soon as those of the chunk before were used up, came
-// back 2 000 clocks later, behind all of the step's tiles.  A chunk's tiles take 1 300 clocks and more from the request to the last line, so that two chunks
-// are on their way while one is worked on: rings of three (of two: 2 350 clocks a step where three take 1 340).
+// back 2 000 clocks later, behind all of the step's tiles.  A chunk's tiles come 1 300 clocks and more after the request, so that two chunks are on
+// their way while one is worked on: rings of three (of two: 2 350 clocks a step where three take 1 340).
 #pragma once
 #include "mdn_gdr.h"
+#include "mdn_scan_rules.h"
 
 namespace mdn {
 
@@ -39,6 +41,49 @@ template <typename T, int D, bool PERMUTED> struct GLoad {
 template <int BYTES> __device__ __forceinline__ void load_block(const void *base, size_t blk, void *to, int w2, int lane) {
     const char *p = static_cast<const char *>(base) + blk * BYTES;
     for (int u = w2; u < BYTES / 1024; u += 2) dma16(p, u * 1024 + lane * 16, lds_addr(to) + u * 1024);
+}
+
+// The operands of chunks further on than the loads, brought into the L2 by the storing waves: four bytes of every 64, each workgroup of a
+// (sequence, head) pair its share of the lanes.  A CU has only so many lines on their way at a time, and all of a pair's workgroups ask for
+// the same ones at the same time, so that every load took as long as one from HBM.
+template <int N> struct GdrTouch { // N: places per lane (none: nothing is brought)
+    const char *at[N ? N : 1];
+    ptrdiff_t step[N ? N : 1];
+    int end[N ? N : 1], p[N ? N : 1]; // a lane's lines are in the chunks before `end`
+    // part: this wave's number among the `parts` storing waves of the pair
+    __device__ __forceinline__ void aim(int part, int parts, int lane) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) p[u] = (u * parts + part) * 64 + lane, end[u] = 0, at[u] = nullptr, step[u] = 0;
+    }
+    // a tensor's share: `rows` rows of `bytes`, `stride` apart, per chunk, the next chunk's `chunk` bytes on; `last`: the last row in the last chunk
+    __device__ __forceinline__ void add(const void *t, int rows, int bytes, ptrdiff_t stride, ptrdiff_t chunk, int chunks, int last) {
+        const int per_row = bytes / 64;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int row = p[u] / per_row;
+            if (p[u] >= 0 && row < rows) {
+                at[u] = static_cast<const char *>(t) + row * stride + p[u] % per_row * 64;
+                step[u] = chunk;
+                end[u] = row > last ? chunks - 1 : chunks;
+            }
+            p[u] -= rows * per_row;
+        }
+    }
+    // (as LDS transfers, which nothing has to wait for: dst is 256 bytes that nobody reads)
+    __device__ __forceinline__ void chunk(int n, const void *dst) const {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            if (n >= 0 && n < end[u])
+                asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dword %0, off"
+                             :
+                             : "v"(at[u] + n * step[u]), "s"(__builtin_amdgcn_readfirstlane((int)lds_addr(dst)))
+                             : "memory", "m0");
+    }
+};
+// places per lane for `lines` lines of 64 bytes and a row of dv elements in each of 64 rows, whether dv is 64 or 128
+constexpr int touch_places(int lines, int bytes, int cols) {
+    const int a = (lines + 64 * bytes - 1) / (64 / cols * 128) + 1, b = (lines + 128 * bytes - 1) / (128 / cols * 128) + 1;
+    return a > b ? a : b;
 }
 
 // Everything asked for so far is there, and the compiler knows: it otherwise waits inside a loop for what was requested in front of it.
@@ -82,9 +127,7 @@ template <typename T, int N> struct Slate {
     }
 };
 
-// Stores of the waves beside the chain go through buffer descriptors: what lies behind the last row, and a tensor that is not wanted (no
-// bytes in reach), is dropped by the bounds check.  With branches around them the compiler cannot count what is on its way behind the
-// loads it waits for, and waits for all of it.
+// Stores go through buffer descriptors: what lies behind the last row is dropped by the bounds check.
 typedef unsigned gdr_u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t out_rows(void *base, size_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(base, 0, (int)bytes, 0x00020000);
@@ -172,6 +215,18 @@ template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void save_s
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int x = 0; x < 4; ++x) g[(size_t)(Gd<T>::row(T0 + t, 4 * kg) + x) * dv + col + r] = S[t][x];
+}
+
+// Whether the forward scan brings later chunks' operands into the L2 (GdrTouch): in 16 bits only where the call moves more than the last-level
+// cache holds one and a half times, whose latency the loads cover.  Forward in us, without / with, 16 heads of 128: 8 192 tokens 146 / 150 (with
+// kept states 155 / 164), 16 384 270 / 276 (387 / 384), 24 576 577 / 531 (719 / 656), 32 768 768 / 708 (947 / 868); 4 x 4 096 135 / 144 (214 / 203).
+// In fp32, where loads are not beside the products, always: 8 192 tokens 557 / 543 (594 / 552).  With remainders never: the chain is what a step
+// waits for (32 768 tokens 857 / 895).  The reverse scan always does, but with remainders; forward and backward pass's backward, 8 192 tokens 260 / 236,
+// 32 768 1 099 / 912, 8 x 2 048 of 8 heads 151 / 138, 8 192 in fp32 1 255 / 1 156.
+inline bool gdr_touch_pays(const GdrDims &d, int key_rows, int value_rows, bool states) {
+    if (d.dtype == 1) return true;
+    const size_t block = 64 * (size_t)(key_rows * d.dk + value_rows * d.dv) * 2 + (states ? (size_t)d.dk * d.dv * 2 : 0);
+    return (size_t)d.nchunks * d.H * block > 3 * kLastLevelCache / 2;
 }
 
 // 16 columns per workgroup while the CUs hold all of those workgroups, or 32

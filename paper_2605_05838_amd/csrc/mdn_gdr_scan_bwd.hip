@@ -1,7 +1,8 @@
 // Gated delta rule, reverse scan.  Per chunk, D the adjoint of the state at its END, from the last chunk to the first, dO' = scale dO:
-//     beside the chain, one chunk ahead:   X = P^T dO',   Y = (e^G Q)^T dO'   (fp32, through LDS); stores of dV and D
+//     beside the chain, one chunk ahead:   X = P^T dO',   Y = (e^G Q)^T dO'   (fp32, through LDS)
 //     chain:   dE = X + e^{G_C - G} beta K D,   dV = T^T dE,   D <- e^{G_C} D + Y - K^T (e^G dV)
-// Two barriers a step: at its start, and when the chain has taken X and Y and the waves beside it have taken the step before's D and dV:
+//     stores of dV and D, one chunk behind
+// Two barriers a step: at its start, and when the chain has taken X and Y and the storing waves have taken the step before's D and dV:
 // then either side writes the next.
 // PRECISE (a call that asks for dS0, which is 32-bit): as in the forward scan; P^T and e^G dO' have remainders as well (dO and Q are exact).
 #include "mdn_gdr_scan.h"
@@ -10,8 +11,11 @@ namespace mdn {
 
 namespace {
 
+// beside the chain, chain, loads, stores
+template <typename T, int NCG> constexpr int bwd_waves() { return 2 + NCG + 2 + (sizeof(T) == 2 ? 2 : 0); }
+
 template <typename T, int DK, int NCG, bool PRECISE>
-__global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
+__global__ __launch_bounds__((bwd_waves<T, NCG>() * 64)) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
     typedef Gd<T> G;
     typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
@@ -21,6 +25,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
     constexpr bool RING = sizeof(T) == 2;    // otherwise loads between two barriers, not beside the products
     // ring depths: what the chain reads; T^T; what the waves beside it read (there is no room for three of everything); coefficients
     constexpr int D = RING ? 3 : 1, DT = PRECISE ? 2 : D, DQ = RING ? 2 : 1, DC = 4;
+    constexpr int LOADS = 2 + NCG, STORES = LOADS + 2; // first waves of each kind
     constexpr int SETS = RING ? 2 : 1; // chunks of P^T that a wave beside the chain has asked for
     typedef GLoad<T, DK, true> LoadK;
     typedef GLoad<T, COLS, false> LoadV;
@@ -28,6 +33,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
     __shared__ __align__(16) float s_c[DC][kGdrCoef];
     __shared__ __align__(16) f32x4 s_x[NCG][4][64], s_y[NCG][NT][64];
     __shared__ __align__(16) T s_s[NCG][SlateS::SIZE], s_r[NCG * SlateE::SIZE];
+    __shared__ __align__(16) int s_touch[2][64];
 
     const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, kg = lane >> 4;
     int bh, sub;
@@ -38,8 +44,41 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
     const unsigned rsv = (unsigned)(d.H * d.dv), rsk = (unsigned)(d.Hk * DK);
 
     // Step n: chunk N - 1 - n on the chain, the one before it (in time) beside it
-    if (w >= 2 + NCG) { // ---- loads
-        const int w2 = w - 2 - NCG;
+    auto store = [&](int n, int w2) { // dV, D of step n
+        const int r = lane & 15, kg = lane >> 4, m = N - 1 - n;
+        const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0, reach = ((size_t)(n == 0 ? last : 63) * rsv + COLS) * sizeof(T);
+        store_tokens<T, NCG, SlateE::LD>(out_rows(static_cast<T *>(a.dv) + at, reach), rsv * (unsigned)sizeof(T), s_r, 32 * w2, 32 * w2, r, kg);
+        store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.dstates) + (q.blk + m) * DK * d.dv, (size_t)DK * d.dv * sizeof(T)), s_s, w2, col0, lane);
+    };
+    // (not with remainders, where the chain is what a step waits for)
+    GdrTouch<PRECISE ? 0 : touch_places(2 * DK * (int)sizeof(T) + 2 * TB / 64 + 16, (int)sizeof(T), COLS)> touch;
+    auto aim_touch = [&](int w2) {
+        touch.aim(sub * 2 + w2, d.dv / COLS * 2, lane);
+        const ptrdiff_t row = rsk * sizeof(T), rov = rsv * sizeof(T);
+        touch.add(static_cast<const T *>(a.k) + q.k * DK, 64, DK * sizeof(T), row, 64 * row, N, last);
+        touch.add(static_cast<const T *>(a.q) + q.k * DK, 64, DK * sizeof(T), row, 64 * row, N, last);
+        touch.add(static_cast<const T *>(a.dO) + q.v * d.dv, 64, d.dv * sizeof(T), rov, 64 * rov, N, last);
+        auto block = [&](const void *t, int bytes) { touch.add(static_cast<const char *>(t) + q.blk * bytes, 1, bytes, 0, bytes, N, 0); };
+        block(a.TT, TB);
+        block(a.PT, TB);
+        block(a.coef, kGdrCoef * 4);
+    };
+    if (w >= STORES) {
+        const int w2 = w - STORES;
+        aim_touch(w2);
+        __syncthreads();
+        __syncthreads();
+        for (int n = 0; n <= N; ++n) {
+            __syncthreads();
+            if (n) store(n - 1, w2);
+            __syncthreads();
+            touch.chunk(N - 1 - n - kTouchAhead, s_touch[w2]);
+        }
+        wait_vm<0>();
+        return;
+    }
+    if (w >= LOADS) {
+        const int w2 = w - LOADS;
         LoadK lk, lk_end;
         LoadV lv, lv_end;
         const T *k = static_cast<const T *>(a.k) + q.k * DK, *qq = static_cast<const T *>(a.q) + q.k * DK;
@@ -62,6 +101,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
         get_q(0);
         wait_vm<0>();
         __syncthreads();
+        if constexpr (!RING) aim_touch(w2);
         if constexpr (RING) {
             get_k(0);
             get_t(0);
@@ -93,9 +133,12 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
                 if (n + 1 < N) get_q(n + 1);
                 wait_vm<0>();
                 __syncthreads();
+                if (n) store(n - 1, w2); // (and stores, while the others multiply)
                 __syncthreads();
+                touch.chunk(N - 1 - n - kTouchAhead, s_touch[w2]);
                 __syncthreads();
             }
+            wait_vm<0>();
         }
         return;
     }
@@ -253,11 +296,6 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
             slot = next_slot<DQ>(slot);
             slot_c = next_slot<DC>(slot_c);
         };
-        auto store = [&](int m, int rows) { // dV, D of chunk m
-            const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0, reach = ((size_t)(rows - 1) * rsv + COLS) * sizeof(T);
-            store_tokens<T, NCG, SlateE::LD>(out_rows(static_cast<T *>(a.dv) + at, reach), rsv * (unsigned)sizeof(T), s_r, 32 * w, 32 * w, r, kg);
-            store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.dstates) + (q.blk + m) * DK * d.dv, (size_t)DK * d.dv * sizeof(T)), s_s, w, col0, lane);
-        };
 #pragma unroll
         for (int i = 0; i < SETS; ++i) fetch(sets[i], i);
         all_arrived();
@@ -266,7 +304,6 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
         __syncthreads();
         auto turn = [&](Set &x, int n) {
             __syncthreads();
-            store(N - n, n == 1 ? last + 1 : 64);
             __syncthreads();
             ahead(x, n + 1);
             if constexpr (!RING) __syncthreads();
@@ -276,7 +313,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
         __syncthreads();
         if (N > 1) ahead(sets[SETS - 1], 1);
         if constexpr (!RING) __syncthreads();
-        // steps 1 .. N - 2, whole turns without a branch inside (see out_rows): X, Y of steps 2 .. N - 1
+        // steps 1 .. N - 2, whole turns without a branch inside (the compiler counts the loads in flight): X, Y of steps 2 .. N - 1
         int n = 1;
         for (; n + SETS <= N - 1; n += SETS)
 #pragma unroll
@@ -285,7 +322,6 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
         // the last two steps: nothing is ahead of them
         for (; n <= N; ++n) {
             __syncthreads();
-            store(N - n, n == 1 ? last + 1 : 64);
             __syncthreads();
             if constexpr (!RING) __syncthreads();
         }
@@ -296,7 +332,7 @@ __global__ __launch_bounds__((NCG + 4) * 64) void gdr_scan_bwd_kernel(GdrDims d,
 
 template <typename T, int DK, int NCG, bool PRECISE> hipError_t launch_cols(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {
     return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, NCG, PRECISE>), grid, dim3((NCG + 4) * 64), 0, s, d, a, first);
+        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, NCG, PRECISE>), grid, dim3((bwd_waves<T, NCG>() * 64)), 0, s, d, a, first);
     });
 }
 template <typename T, int DK, bool PRECISE> hipError_t launch(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {

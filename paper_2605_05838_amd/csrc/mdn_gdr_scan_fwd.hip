@@ -1,7 +1,8 @@
 // Gated delta rule, forward scan and reconstruction of the chunk-start states.  Per chunk, S the state at its start:
 //     chain:   E = T (V - e^G K S),   S <- e^{G_C} S + K^T (e^{G_C - G} beta E)
-//     beside it, one chunk behind:   O = scale (e^G Q S + P E); stores of O, E and S
-// S and E reach the waves beside the chain through LDS, rounded to the storage type.
+//     beside it, one chunk behind:   O = scale (e^G Q S + P E)
+//     stores of E and S one chunk behind the chain, of O two
+// S, E and O pass from wave to wave through LDS, rounded to the storage type.
 // Bounds: HBM where all CUs have a workgroup.  Below, the CU's loads: 16 KB each of K and Q, 6 of T and P, 1 KB of V per 8 columns a step,
 // of which a CU takes 25 to 37 B a clock.
 // PRECISE (a call that asks for the final states, which are 32-bit): S, T, V - e^G K S and e^{G_C - G} beta E enter their products as value +
@@ -17,15 +18,21 @@ namespace {
 // ([4, 4 096] tokens, 16 heads, d = 128), where one wave's products are done before the chunk behind them is there.
 template <typename T, int NCG, bool PRECISE> constexpr int CW = sizeof(T) == 4 || (PRECISE && NCG == 1) ? 2 : 1;
 
+// beside the chain, chain, loads, stores
+template <typename T, int NCG, bool PRECISE, bool REBUILD> constexpr int fwd_waves() {
+    return (REBUILD ? 0 : 2) + CW<T, NCG, PRECISE> * NCG + 2 + (sizeof(T) == 2 ? 2 : 0);
+}
+
 // REBUILD: E is given (in v's place), only the states are wanted.  KEEP: E or the states are.
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP>
-__global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
+__global__ __launch_bounds__((fwd_waves<T, NCG, PRECISE, REBUILD>() * 64)) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
     typedef Gd<T> G;
     typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
     typedef Slate<T, 64> SlateE;
     constexpr int NT = DK / 16, SK = DK / G::KS, S64 = 64 / G::KS, COLS = 16 * NCG, TRI = G::NF * 64 * G::E;
     constexpr int CWS = CW<T, NCG, PRECISE>, NS = CWS + 1; // NS: slots of S
+    constexpr int CHAIN = REBUILD ? 0 : 2, LOADS = CHAIN + CWS * NCG, STORES = LOADS + 2; // first waves of each kind
     constexpr int TB = TRI * (int)sizeof(T);  // bytes of a triangle
     constexpr int LDO = 32 + G::E;            // row length of what a wave beside the chain stores: 32 tokens of all columns, whole rows
     constexpr int D = sizeof(T) == 2 ? 3 : 1; // ring depth; 1: loads between two barriers, not beside the products
@@ -38,8 +45,9 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
     // S: with two waves, read by the other one when it is new, beside the chain a step later, and written for the step after that meanwhile
     __shared__ __align__(16) T s_s[NS][NCG][SlateS::SIZE], s_sl[NCG][CWS == 2 && PRECISE ? SlateS::SIZE : 8];
     __shared__ __align__(16) Frag s_x[NCG][CWS == 2 ? S64 : 1][64], s_xl[NCG][CWS == 2 && PRECISE ? S64 : 1][64]; // V - e^G K S, from wave to wave
+    __shared__ __align__(16) int s_touch[2][64];
     __shared__ int s_said[NCG][2]; // steps whose half of it is there
-    __shared__ __align__(16) T s_e[2][REBUILD ? 8 : NCG * SlateE::SIZE], s_o[2][REBUILD ? 8 : COLS * LDO];
+    __shared__ __align__(16) T s_e[2][REBUILD ? 8 : NCG * SlateE::SIZE], s_o[2][2][REBUILD ? 8 : COLS * LDO];
 
     const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, kg = lane >> 4;
     int bh, sub;
@@ -49,9 +57,54 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
     const int col0 = sub * COLS, N = q.n, last = (q.len - 1) & 63; // last: the last row of the last chunk
     const unsigned rsv = (unsigned)(d.H * d.dv), rsk = (unsigned)(d.Hk * DK);
 
-    // Step n: chunk n on the chain, chunk n - 1 beside it
-    if (w >= 2 + CWS * NCG) { // ---- loads
-        const int w2 = w - 2 - CWS * NCG;
+    // Step n: chunk n on the chain, chunk n - 1 beside it; by the two waves w2 = 0, 1 that store: S, E of chunk n - 1, O of chunk n - 2
+    auto store = [&](int n, int w2) {
+        const int r = lane & 15, kg = lane >> 4;
+        auto rows = [&](void *to, int m) {
+            const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0;
+            return out_rows(static_cast<T *>(to) + at, to ? ((size_t)(m == N - 1 ? last : 63) * rsv + COLS) * sizeof(T) : 0);
+        };
+        if constexpr (KEEP) {
+            if (n >= 1 && n <= N) {
+                const int m = n - 1;
+                if constexpr (!REBUILD)
+                    if (a.e) store_tokens<T, NCG, SlateE::LD>(rows(a.e, m), rsv * (unsigned)sizeof(T), s_e[m & 1], 32 * w2, 32 * w2, r, kg);
+                if (a.states)
+                    store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.states) + (q.blk + m) * DK * d.dv, (size_t)DK * d.dv * sizeof(T)), s_s[m % NS], w2,
+                                            col0, lane);
+            }
+        }
+        if constexpr (!REBUILD)
+            if (n >= 2) store_tokens<T, NCG, LDO>(rows(a.o, n - 2), rsv * (unsigned)sizeof(T), s_o[n & 1][w2], 0, 32 * w2, r, kg);
+    };
+    GdrTouch<PRECISE ? 0 : touch_places((2 - REBUILD) * DK * (int)sizeof(T) + (REBUILD ? 0 : 2) * TB / 64 + 16, (int)sizeof(T), COLS)> touch;
+    auto aim_touch = [&](int w2) {
+        touch.aim(sub * 2 + w2, d.dv / COLS * 2, lane);
+        if (!a.touch) return;
+        const ptrdiff_t row = rsk * sizeof(T), rov = rsv * sizeof(T);
+        touch.add(static_cast<const T *>(a.k) + q.k * DK, 64, DK * sizeof(T), row, 64 * row, N, last);
+        touch.add(static_cast<const T *>(a.v) + q.v * d.dv, 64, d.dv * sizeof(T), rov, 64 * rov, N, last);
+        auto block = [&](const void *t, int bytes) { touch.add(static_cast<const char *>(t) + q.blk * bytes, 1, bytes, 0, bytes, N, 0); };
+        if constexpr (!REBUILD) {
+            touch.add(static_cast<const T *>(a.q) + q.k * DK, 64, DK * sizeof(T), row, 64 * row, N, last);
+            block(a.T, TB);
+            block(a.P, TB);
+        }
+        block(a.coef, kGdrCoef * 4);
+    };
+    if (w >= STORES) {
+        const int w2 = w - STORES;
+        aim_touch(w2);
+        for (int n = 0; n <= N + 1; ++n) {
+            __syncthreads();
+            store(n, w2);
+            touch.chunk(n + kTouchAhead, s_touch[w2]);
+        }
+        wait_vm<0>();
+        return;
+    }
+    if (w >= LOADS) {
+        const int w2 = w - LOADS;
         LoadK lk, lk_end;
         LoadV lv, lv_end;
         const T *k = static_cast<const T *>(a.k) + q.k * DK, *v = static_cast<const T *>(a.v) + q.v * d.dv + col0;
@@ -67,12 +120,16 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
             if constexpr (PRECISE) load_block<TB>(a.T_lo, q.blk + n, s_tl[n % D], w2, lane);
         };
         if constexpr (D == 1) {
-            for (int n = 0; n <= N; ++n) {
+            aim_touch(w2);
+            for (int n = 0; n <= N + 1; ++n) { // (and stores, while the others multiply)
                 if (n < N) request(n);
                 wait_vm<0>();
                 __syncthreads();
+                store(n, w2);
+                touch.chunk(n + kTouchAhead, s_touch[w2]);
                 __syncthreads();
             }
+            wait_vm<0>();
         } else {
             // requests of a chunk by either wave (the first one's coefficients included)
             constexpr int C1 = LoadK::COUNT + LoadV::COUNT + (REBUILD ? 0 : TB / 2048) + (PRECISE ? TB / 2048 : 0), C0 = C1 + 1;
@@ -84,7 +141,7 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
             } else {
                 wait_vm<0>();
             }
-            for (int n = 0; n <= N; ++n) {
+            for (int n = 0; n <= N + 1; ++n) {
                 __syncthreads();
                 if (n + 2 < N) {
                     request(n + 2);
@@ -101,7 +158,7 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
     auto chain = [&](auto half) {
         // this wave's half (or all): of dk and of the tokens
         constexpr int TW = decltype(half)::value, HT = NT / CWS, HS = SK / CWS, H64 = S64 / CWS, RT = 4 / CWS;
-        const int cg = (w - 2) / CWS, col = col0 + 16 * cg;
+        const int cg = (w - CHAIN) / CWS, col = col0 + 16 * cg;
         int slot = 0, slot_c = 0, slot_s = 0;
         f32x4 S[HT];
         Frags<T, HT, PRECISE> Sb;
@@ -117,7 +174,7 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
         Sb.from(S);
         if constexpr (CWS == 2) publish();
         if (lane == 0) s_said[cg][TW] = 0;
-        for (int n = 0; n <= N; ++n) {
+        for (int n = 0; n <= N + 1; ++n) {
             __syncthreads();
             if (n < N) {
                 const T *k = s_k[slot], *v = s_v[slot], *tri = s_t[slot], *tri_lo = s_tl[slot];
@@ -216,7 +273,7 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
         }
         if (a.S_final) save_state<T, TW * HT>(S, a.S_final + q.state * DK * d.dv, d.dv, col, r, kg);
     };
-    if (w >= 2) { // ---- the chain
+    if (w >= CHAIN) { // ---- the chain
         if (CWS == 1 || w % 2 == 0) chain(std::integral_constant<int, 0>{});
         else chain(std::integral_constant<int, CWS - 1>{});
         return;
@@ -251,61 +308,48 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
         };
         int slot_s = 0;
         auto step = [&](Set &x, int m) {
-            const int rows = m == N - 1 ? last + 1 : 64;
-            if constexpr (!REBUILD) {
-                const T *se = s_e[m & 1];
-                const float *c = s_c[slot_c] + G::row(0, 4 * kg);
-                f32x4 O[NCG][2];
+            const T *se = s_e[m & 1];
+            const float *c = s_c[slot_c] + G::row(0, 4 * kg);
+            f32x4 O[NCG][2];
 #pragma unroll
-                for (int g = 0; g < NCG; ++g) zero_acc(O[g]);
+            for (int g = 0; g < NCG; ++g) zero_acc(O[g]);
 #pragma unroll
-                for (int s = 0; s < SK; ++s)
-#pragma unroll
-                    for (int g = 0; g < NCG; ++g) {
-                        const Frag b = SlateS::get(s_s[slot_s][g], s, r, kg);
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) O[g][t] = gd_mma<T>(x.q[t][s], b, O[g][t]);
-                    }
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int g = 0; g < NCG; ++g) O[g][t] *= *reinterpret_cast<const f32x4 *>(c + G::row(T0 + t, 0));
-#pragma unroll
-                for (int s = 0; s < S64; ++s)
-#pragma unroll
-                    for (int g = 0; g < NCG; ++g) {
-                        if (s > G::last(T0 + 1)) continue;
-                        const Frag b = SlateE::get(se + g * SlateE::SIZE, s, r, kg);
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-                            if (s <= G::last(T0 + t)) O[g][t] = gd_mma<T>(x.p[t][s], b, O[g][t]);
-                    }
-                fetch(x, m + SETS);
+            for (int s = 0; s < SK; ++s)
 #pragma unroll
                 for (int g = 0; g < NCG; ++g) {
+                    const Frag b = SlateS::get(s_s[slot_s][g], s, r, kg);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) O[g][t] *= d.scale;
-#pragma unroll
-                    for (int s = 0; s < 2 / G::KT; ++s)
-                        *reinterpret_cast<Frag *>(s_o[w] + (16 * g + r) * LDO + s * G::KS + kg * G::E) = G::frag(&O[g][s * G::KT]);
+                    for (int t = 0; t < 2; ++t) O[g][t] = gd_mma<T>(x.q[t][s], b, O[g][t]);
                 }
-                const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0, reach = ((size_t)(rows - 1) * rsv + COLS) * sizeof(T);
-                store_tokens<T, NCG, LDO>(out_rows(static_cast<T *>(a.o) + at, reach), rsv * (unsigned)sizeof(T), s_o[w], 0, 32 * w, r, kg);
-                if constexpr (KEEP)
-                    store_tokens<T, NCG, SlateE::LD>(out_rows(static_cast<T *>(a.e) + at, a.e ? reach : 0), rsv * (unsigned)sizeof(T), se, 32 * w,
-                                                     32 * w, r, kg);
-                slot_c = next_slot<DC>(slot_c);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int g = 0; g < NCG; ++g) O[g][t] *= *reinterpret_cast<const f32x4 *>(c + G::row(T0 + t, 0));
+#pragma unroll
+            for (int s = 0; s < S64; ++s)
+#pragma unroll
+                for (int g = 0; g < NCG; ++g) {
+                    if (s > G::last(T0 + 1)) continue;
+                    const Frag b = SlateE::get(se + g * SlateE::SIZE, s, r, kg);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        if (s <= G::last(T0 + t)) O[g][t] = gd_mma<T>(x.p[t][s], b, O[g][t]);
+                }
+            fetch(x, m + SETS);
+#pragma unroll
+            for (int g = 0; g < NCG; ++g) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) O[g][t] *= d.scale;
+#pragma unroll
+                for (int s = 0; s < 2 / G::KT; ++s)
+                    *reinterpret_cast<Frag *>(s_o[m & 1][w] + (16 * g + r) * LDO + s * G::KS + kg * G::E) = G::frag(&O[g][s * G::KT]);
             }
-            if constexpr (KEEP)
-                store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.states) + (q.blk + m) * DK * d.dv, a.states ? (size_t)DK * d.dv * sizeof(T) : 0),
-                                        s_s[slot_s], w, col0, lane);
+            slot_c = next_slot<DC>(slot_c);
             slot_s = next_slot<NS>(slot_s);
         };
-        if constexpr (!REBUILD) {
 #pragma unroll
-            for (int i = 0; i < SETS; ++i) fetch(sets[i], i);
-            all_arrived();
-        }
+        for (int i = 0; i < SETS; ++i) fetch(sets[i], i);
+        all_arrived();
         __syncthreads();
         if constexpr (D == 1) __syncthreads();
         auto turn = [&](Set &x, int m) {
@@ -314,18 +358,22 @@ __global__ __launch_bounds__((CW<T, NCG, PRECISE> * NCG + 4) * 64) void gdr_scan
             if constexpr (D == 1) __syncthreads();
         };
         int m = 0;
-        for (; m + SETS <= N; m += SETS) // (whole turns, without a branch inside: see out_rows)
+        for (; m + SETS <= N; m += SETS) // (whole turns, without a branch inside: the compiler counts the loads in flight)
 #pragma unroll
             for (int i = 0; i < SETS; ++i) turn(sets[i], m + i);
         if (m < N) turn(sets[0], m);
+        __syncthreads();
+        if constexpr (D == 1) __syncthreads();
     };
-    if (w == 0) beside(std::integral_constant<int, 0>{});
-    else beside(std::integral_constant<int, 2>{});
+    if constexpr (!REBUILD) {
+        if (w == 0) beside(std::integral_constant<int, 0>{});
+        else beside(std::integral_constant<int, 2>{});
+    }
 }
 
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP> hipError_t launch_keep(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
     return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, NCG, PRECISE, REBUILD, KEEP>), grid, dim3((CW<T, NCG, PRECISE> * NCG + 4) * 64), 0, s, d, a, first);
+        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, NCG, PRECISE, REBUILD, KEEP>), grid, dim3((fwd_waves<T, NCG, PRECISE, REBUILD>() * 64)), 0, s, d, a, first);
     });
 }
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD> hipError_t launch_cols(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
@@ -338,13 +386,17 @@ template <typename T, int DK, bool PRECISE, bool REBUILD> hipError_t launch(cons
 
 } // namespace
 
-hipError_t launch_gdr_scan_fwd(const GdrDims &d, const GdrScanFwdArgs &a, bool precise, hipStream_t s) {
+hipError_t launch_gdr_scan_fwd(const GdrDims &d, const GdrScanFwdArgs &args, bool precise, hipStream_t s) {
+    GdrScanFwdArgs a = args;
+    a.touch = gdr_touch_pays(d, 2, args.e ? 3 : 2, args.states);
     if (d.dtype == 1) return d.dk == 64 ? launch<float, 64, false, false>(d, a, s) : launch<float, 128, false, false>(d, a, s);
     if (precise) return d.dk == 64 ? launch<bf16_t, 64, true, false>(d, a, s) : launch<bf16_t, 128, true, false>(d, a, s);
     return d.dk == 64 ? launch<bf16_t, 64, false, false>(d, a, s) : launch<bf16_t, 128, false, false>(d, a, s);
 }
 
-hipError_t launch_gdr_rebuild(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
+hipError_t launch_gdr_rebuild(const GdrDims &d, const GdrScanFwdArgs &args, hipStream_t s) {
+    GdrScanFwdArgs a = args;
+    a.touch = gdr_touch_pays(d, 1, 1, true);
     if (d.dtype == 1) return d.dk == 64 ? launch<float, 64, false, true>(d, a, s) : launch<float, 128, false, true>(d, a, s);
     return d.dk == 64 ? launch<bf16_t, 64, false, true>(d, a, s) : launch<bf16_t, 128, false, true>(d, a, s);
 }
