@@ -5,7 +5,8 @@
 //   2 waves       beside the chain: what hangs on it without being part of it;
 //   NCG waves     the chain: the state in their accumulators (see mdn_gdr.h); in fp32 and with remainders, forward, two waves to 16 columns;
 //   2 waves       loads: the chunks ahead, HBM -> LDS without registers, into rings;
-//   2 waves       stores, out of LDS, and lines for later (GdrTouch); in fp32 the loading waves, whose loads are not beside the products.
+//   2 waves       stores, out of LDS, and lines for later (GdrTouch); without rings (gdr_ring) the loading waves, whose loads are then not
+//                 beside the products.
 // A chain wave is bound by its LDS instructions, ~26 clocks each, most of them reads of A operands: 2 050 clocks a step at d = 128 in 16
 // bits, 3 650 with remainders.  Two waves to 16 columns each form the products of half of the tokens with the whole state, whose other half
 // they find in LDS since the step's barrier, hand them to the other one, and then have all they need for half of the next state; the small
@@ -18,6 +19,9 @@
 #include "mdn_scan_rules.h"
 
 namespace mdn {
+
+// Whether LDS holds rings of chunks: not for 32-bit rows of 128, or of 64 with 32 columns.
+template <typename T, int DK, int NCG> constexpr bool gdr_ring() { return sizeof(T) == 2 || (DK == 64 && NCG == 1); }
 
 // The tiles of a chunk that the loading waves (w2 = 0, 1) bring: [64][D] rows, permuted as GTile<T, LAYOUT> says
 template <typename T, int D, bool PERMUTED> struct GLoad {

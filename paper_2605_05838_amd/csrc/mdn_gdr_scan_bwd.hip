@@ -12,21 +12,21 @@ namespace mdn {
 namespace {
 
 // beside the chain, chain, loads, stores
-template <typename T, int NCG> constexpr int bwd_waves() { return 2 + NCG + 2 + (sizeof(T) == 2 ? 2 : 0); }
+template <typename T, int DK, int NCG> constexpr int bwd_waves() { return 2 + NCG + 2 + (gdr_ring<T, DK, NCG>() ? 2 : 0); }
 
 template <typename T, int DK, int NCG, bool PRECISE>
-__global__ __launch_bounds__((bwd_waves<T, NCG>() * 64)) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
+__global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
     typedef Gd<T> G;
     typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
     typedef Slate<T, 64> SlateE;
     constexpr int NT = DK / 16, SK = DK / G::KS, S64 = 64 / G::KS, COLS = 16 * NCG, TRI = G::NF * 64 * G::E;
     constexpr int TB = TRI * (int)sizeof(T); // bytes of a triangle
-    constexpr bool RING = sizeof(T) == 2;    // otherwise loads between two barriers, not beside the products
+    constexpr bool RING = gdr_ring<T, DK, NCG>(); // otherwise loads between two barriers, not beside the products
     // ring depths: what the chain reads; T^T; what the waves beside it read (there is no room for three of everything); coefficients
     constexpr int D = RING ? 3 : 1, DT = PRECISE ? 2 : D, DQ = RING ? 2 : 1, DC = 4;
     constexpr int LOADS = 2 + NCG, STORES = LOADS + 2; // first waves of each kind
-    constexpr int SETS = RING ? 2 : 1; // chunks of P^T that a wave beside the chain has asked for
+    constexpr int SETS = sizeof(T) == 2 ? 2 : 1; // chunks of P^T that a wave beside the chain has asked for
     typedef GLoad<T, DK, true> LoadK;
     typedef GLoad<T, COLS, false> LoadV;
     __shared__ __align__(16) T s_k[D][64 * DK], s_q[DQ][64 * DK], s_do[DQ][64 * COLS], s_t[DT][TRI], s_tl[DT][PRECISE ? TRI : 8];
@@ -165,7 +165,7 @@ __global__ __launch_bounds__((bwd_waves<T, NCG>() * 64)) void gdr_scan_bwd_kerne
                         ec[t] = *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 0));
                     }
                 };
-                if (RING) decays(); // (32-bit storage has no registers for them yet)
+                if (RING) decays(); // (32-bit rows of 128 leave no registers for them yet)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) X[t] = s_x[cg][t][lane];
                 Frags<T, NT, PRECISE> Sb;
@@ -332,7 +332,7 @@ __global__ __launch_bounds__((bwd_waves<T, NCG>() * 64)) void gdr_scan_bwd_kerne
 
 template <typename T, int DK, int NCG, bool PRECISE> hipError_t launch_cols(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {
     return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, NCG, PRECISE>), grid, dim3((bwd_waves<T, NCG>() * 64)), 0, s, d, a, first);
+        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, NCG, PRECISE>), grid, dim3((bwd_waves<T, DK, NCG>() * 64)), 0, s, d, a, first);
     });
 }
 template <typename T, int DK, bool PRECISE> hipError_t launch(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {

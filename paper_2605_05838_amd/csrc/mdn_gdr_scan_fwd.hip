@@ -19,13 +19,13 @@ namespace {
 template <typename T, int NCG, bool PRECISE> constexpr int CW = sizeof(T) == 4 || (PRECISE && NCG == 1) ? 2 : 1;
 
 // beside the chain, chain, loads, stores
-template <typename T, int NCG, bool PRECISE, bool REBUILD> constexpr int fwd_waves() {
-    return (REBUILD ? 0 : 2) + CW<T, NCG, PRECISE> * NCG + 2 + (sizeof(T) == 2 ? 2 : 0);
+template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD> constexpr int fwd_waves() {
+    return (REBUILD ? 0 : 2) + CW<T, NCG, PRECISE> * NCG + 2 + (gdr_ring<T, DK, NCG>() ? 2 : 0);
 }
 
 // REBUILD: E is given (in v's place), only the states are wanted.  KEEP: E or the states are.
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP>
-__global__ __launch_bounds__((fwd_waves<T, NCG, PRECISE, REBUILD>() * 64)) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
+__global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) void gdr_scan_fwd_kernel(GdrDims d, GdrScanFwdArgs a, int first) {
     typedef Gd<T> G;
     typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
@@ -35,7 +35,7 @@ __global__ __launch_bounds__((fwd_waves<T, NCG, PRECISE, REBUILD>() * 64)) void 
     constexpr int CHAIN = REBUILD ? 0 : 2, LOADS = CHAIN + CWS * NCG, STORES = LOADS + 2; // first waves of each kind
     constexpr int TB = TRI * (int)sizeof(T);  // bytes of a triangle
     constexpr int LDO = 32 + G::E;            // row length of what a wave beside the chain stores: 32 tokens of all columns, whole rows
-    constexpr int D = sizeof(T) == 2 ? 3 : 1; // ring depth; 1: loads between two barriers, not beside the products
+    constexpr int D = gdr_ring<T, DK, NCG>() ? 3 : 1; // ring depth; 1: loads between two barriers, not beside the products
     constexpr int DC = D + 1;                 // of the coefficients, which both kinds of waves read
     constexpr int SETS = sizeof(T) == 2 ? 2 : 1; // chunks of q and P that a wave beside the chain has asked for
     typedef GLoad<T, DK, true> LoadK;
@@ -373,7 +373,7 @@ __global__ __launch_bounds__((fwd_waves<T, NCG, PRECISE, REBUILD>() * 64)) void 
 
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD, bool KEEP> hipError_t launch_keep(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
     return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, NCG, PRECISE, REBUILD, KEEP>), grid, dim3((fwd_waves<T, NCG, PRECISE, REBUILD>() * 64)), 0, s, d, a, first);
+        hipLaunchKernelGGL((gdr_scan_fwd_kernel<T, DK, NCG, PRECISE, REBUILD, KEEP>), grid, dim3((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)), 0, s, d, a, first);
     });
 }
 template <typename T, int DK, int NCG, bool PRECISE, bool REBUILD> hipError_t launch_cols(const GdrDims &d, const GdrScanFwdArgs &a, hipStream_t s) {
