@@ -142,22 +142,22 @@ template <int AUX, typename V> __device__ __forceinline__ void put16(__amdgpu_bu
 
 // NG slates of LD rows, one after the other -> 32 tokens from token t0 on of a chunk of a [tokens, H, dv] tensor (`to`: from its first
 // row and the first of the 16 NG columns on; rs: bytes between rows), whole rows of these columns at a time (32 bytes of a row and, later,
-// the other 32 cost HBM two writes)
-template <typename T, int NG, int LD>
+// the other 32 cost HBM two writes).  AUX: 2 for non-temporal
+template <typename T, int NG, int LD, int AUX = 2>
 __device__ __forceinline__ void store_tokens(__amdgpu_buffer_rsrc_t to, unsigned rs, const T *slates, int slate_t0, int t0, int r, int kg) {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const int pc = NG == 2 ? kg : kg & 1, tok = 16 * (NG == 2 ? i : kg >> 1) + r; // 16-byte piece of the row, token
             const T *p = slates + (8 * pc + (r >> 2)) * LD + slate_t0 + tok - r + 4 * (r & 3);
-            put16<2>(to, (unsigned)(t0 + tok) * rs + 16 * pc, tr_pair(p, p + 4 * LD));
+            put16<AUX>(to, (unsigned)(t0 + tok) * rs + 16 * pc, tr_pair(p, p + 4 * LD));
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int pc = kg; pc < 4 * NG; pc += 4)
-                put16<2>(to, (unsigned)(t0 + 16 * i + r) * rs + 16 * pc, column4(slates, LD, 4 * pc, slate_t0 + 16 * i, r));
+                put16<AUX>(to, (unsigned)(t0 + 16 * i + r) * rs + 16 * pc, column4(slates, LD, 4 * pc, slate_t0 + 16 * i, r));
     }
 }
 
@@ -221,8 +221,8 @@ template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void save_s
         for (int x = 0; x < 4; ++x) g[(size_t)(Gd<T>::row(T0 + t, 4 * kg) + x) * dv + col + r] = S[t][x];
 }
 
-// Whether the forward scan brings later chunks' operands into the L2 (GdrTouch): in 16 bits only where the call moves more than the last-level
-// cache holds one and a half times, whose latency the loads cover.  Forward in us, without / with, 16 heads of 128: 8 192 tokens 146 / 150 (with
+// Whether the forward scan brings later chunks' operands into the L2 (GdrTouch): in 16 bits only where the rows and states of the call are
+// more than one and a quarter times what the last-level cache holds, whose latency the loads cover.  Forward in us, without / with, 16 heads of 128: 8 192 tokens 146 / 150 (with
 // kept states 155 / 164), 16 384 270 / 276 (387 / 384), 24 576 577 / 531 (719 / 656), 32 768 768 / 708 (947 / 868); 4 x 4 096 135 / 144 (214 / 203).
 // In fp32, where loads are not beside the products, always: 8 192 tokens 557 / 543 (594 / 552).  With remainders never: the chain is what a step
 // waits for (32 768 tokens 857 / 895).  The reverse scan always does, but with remainders; forward and backward pass's backward, 8 192 tokens 260 / 236,
@@ -230,7 +230,7 @@ template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void save_s
 inline bool gdr_touch_pays(const GdrDims &d, int key_rows, int value_rows, bool states) {
     if (d.dtype == 1) return true;
     const size_t block = 64 * (size_t)(key_rows * d.dk + value_rows * d.dv) * 2 + (states ? (size_t)d.dk * d.dv * 2 : 0);
-    return (size_t)d.nchunks * d.H * block > 3 * kLastLevelCache / 2;
+    return (size_t)d.nchunks * d.H * block > 5 * kLastLevelCache / 4;
 }
 
 // 16 columns per workgroup while the CUs hold all of those workgroups, or 32

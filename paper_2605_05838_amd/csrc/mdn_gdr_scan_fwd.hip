@@ -59,23 +59,29 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
 
     // Step n: chunk n on the chain, chunk n - 1 beside it; by the two waves w2 = 0, 1 that store: S, E of chunk n - 1, O of chunk n - 2
     auto store = [&](int n, int w2) {
-        const int r = lane & 15, kg = lane >> 4;
-        auto rows = [&](void *to, int m) {
+        // Non-temporal, but not the 32 bytes of 16 columns where later chunks are brought into the L2: these then wait there for the rest of their
+        // line.  16 heads of 128 in us, non-temporal / not: 32 768 tokens 708 / 676, with kept states 868 / 829; where nothing is brought,
+        // 16 384 268 / 331, and with 32 columns, 4 x 4 096, 82 / 104, the other way.
+        auto tokens = [&](auto ld, void *to, int m, const T *slates, int slate_t0, int w2) {
             const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0;
-            return out_rows(static_cast<T *>(to) + at, to ? ((size_t)(m == N - 1 ? last : 63) * rsv + COLS) * sizeof(T) : 0);
+            const auto rows = out_rows(static_cast<T *>(to) + at, ((size_t)(m == N - 1 ? last : 63) * rsv + COLS) * sizeof(T));
+            const unsigned rs = rsv * (unsigned)sizeof(T);
+            const int r = lane & 15, kg = lane >> 4;
+            if (sizeof(T) == 2 && NCG == 1 && a.touch) store_tokens<T, NCG, decltype(ld)::value, 0>(rows, rs, slates, slate_t0, 32 * w2, r, kg);
+            else store_tokens<T, NCG, decltype(ld)::value>(rows, rs, slates, slate_t0, 32 * w2, r, kg);
         };
         if constexpr (KEEP) {
             if (n >= 1 && n <= N) {
                 const int m = n - 1;
                 if constexpr (!REBUILD)
-                    if (a.e) store_tokens<T, NCG, SlateE::LD>(rows(a.e, m), rsv * (unsigned)sizeof(T), s_e[m & 1], 32 * w2, 32 * w2, r, kg);
+                    if (a.e) tokens(std::integral_constant<int, SlateE::LD>{}, a.e, m, s_e[m & 1], 32 * w2, w2);
                 if (a.states)
                     store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.states) + (q.blk + m) * DK * d.dv, (size_t)DK * d.dv * sizeof(T)), s_s[m % NS], w2,
                                             col0, lane);
             }
         }
         if constexpr (!REBUILD)
-            if (n >= 2) store_tokens<T, NCG, LDO>(rows(a.o, n - 2), rsv * (unsigned)sizeof(T), s_o[n & 1][w2], 0, 32 * w2, r, kg);
+            if (n >= 2) tokens(std::integral_constant<int, LDO>{}, a.o, n - 2, s_o[n & 1][w2], 0, w2);
     };
     GdrTouch<PRECISE ? 0 : touch_places((2 - REBUILD) * DK * (int)sizeof(T) + (REBUILD ? 0 : 2) * TB / 64 + 16, (int)sizeof(T), COLS)> touch;
     auto aim_touch = [&](int w2) {
@@ -388,7 +394,7 @@ template <typename T, int DK, bool PRECISE, bool REBUILD> hipError_t launch(cons
 
 hipError_t launch_gdr_scan_fwd(const GdrDims &d, const GdrScanFwdArgs &args, bool precise, hipStream_t s) {
     GdrScanFwdArgs a = args;
-    a.touch = gdr_touch_pays(d, 2, args.e ? 3 : 2, args.states);
+    a.touch = !precise && gdr_touch_pays(d, 2, args.e ? 3 : 2, args.states);
     if (d.dtype == 1) return d.dk == 64 ? launch<float, 64, false, false>(d, a, s) : launch<float, 128, false, false>(d, a, s);
     if (precise) return d.dk == 64 ? launch<bf16_t, 64, true, false>(d, a, s) : launch<bf16_t, 128, true, false>(d, a, s);
     return d.dk == 64 ? launch<bf16_t, 64, false, false>(d, a, s) : launch<bf16_t, 128, false, false>(d, a, s);
