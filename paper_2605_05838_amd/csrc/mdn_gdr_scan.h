@@ -3,7 +3,7 @@
 // A workgroup walks the chunks of one (sequence, value head) pair for NCG groups of 16 columns of the state, one step per chunk, with
 // four kinds of waves:
 //   2 waves       beside the chain: what hangs on it without being part of it;
-//   NCG waves     the chain: the state in their accumulators (see mdn_gdr.h); in fp32 and with remainders, forward, two waves to 16 columns;
+//   NCG waves     the chain: the state in their accumulators (see mdn_gdr.h); in fp32 and with remainders two waves to 16 columns (CW);
 //   2 waves       loads: the chunks ahead, HBM -> LDS without registers, into rings;
 //   2 waves       stores, out of LDS, and lines for later (GdrTouch); without rings (gdr_ring) the loading waves, whose loads are then not
 //                 beside the products.
@@ -11,9 +11,9 @@
 // bits, 3 650 with remainders.  Two waves to 16 columns each form the products of half of the tokens with the whole state, whose other half
 // they find in LDS since the step's barrier, hand them to the other one, and then have all they need for half of the next state; the small
 // products with T in between both form.
-// The chain loads nothing: the fragments of T, asked for by the wave that wants them as soon as those of the chunk before were used up, came
-// back 2 000 clocks later, behind all of the step's tiles.  A chunk's tiles come 1 300 clocks and more after the request, so that two chunks are on
-// their way while one is worked on: rings of three (of two: 2 350 clocks a step where three take 1 340).
+// The chain loads nothing: the fragments of T, asked for by the wave that wants them as soon as those of the chunk before were used up,
+// came back 2 000 clocks later, behind all of the step's tiles.  A chunk's tiles come 1 300 clocks and more after the request, so that two
+// chunks are on their way while one is worked on: rings of three (of two: 2 350 clocks a step where three take 1 340).
 #pragma once
 #include "mdn_gdr.h"
 #include "mdn_scan_rules.h"
@@ -59,7 +59,8 @@ template <int N> struct GdrTouch { // N: places per lane (none: nothing is broug
 #pragma unroll
         for (int u = 0; u < N; ++u) p[u] = (u * parts + part) * 64 + lane, end[u] = 0, at[u] = nullptr, step[u] = 0;
     }
-    // a tensor's share: `rows` rows of `bytes`, `stride` apart, per chunk, the next chunk's `chunk` bytes on; `last`: the last row in the last chunk
+    // a tensor's share: `rows` rows of `bytes`, `stride` apart, per chunk, the next chunk's `chunk` bytes on; `last`: the last row of the
+    // last chunk
     __device__ __forceinline__ void add(const void *t, int rows, int bytes, ptrdiff_t stride, ptrdiff_t chunk, int chunks, int last) {
         const int per_row = bytes / 64;
 #pragma unroll
@@ -195,8 +196,8 @@ __device__ __forceinline__ void store_state(__amdgpu_buffer_rsrc_t block, const 
     }
 }
 
-// Two waves of the same 16 columns wait for each other: `mine` says that this one's fragments of step n are in LDS (a wave's LDS operations are
-// done in order), and it goes on when the other one's are.  Both are waves of one workgroup: the wait ends.
+// Two waves of the same 16 columns wait for each other: `mine` says that this one's fragments of step n are in LDS (a wave's LDS
+// operations are done in order), and it goes on when the other one's are.  Both are waves of one workgroup: the wait ends.
 __device__ __forceinline__ void say(int *mine, int n) {
     asm volatile("" : : : "memory");
     *const_cast<volatile int *>(mine) = n + 1;
@@ -221,12 +222,12 @@ template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void save_s
         for (int x = 0; x < 4; ++x) g[(size_t)(Gd<T>::row(T0 + t, 4 * kg) + x) * dv + col + r] = S[t][x];
 }
 
-// Whether the forward scan brings later chunks' operands into the L2 (GdrTouch): in 16 bits only where the rows and states of the call are
-// more than one and a quarter times what the last-level cache holds, whose latency the loads cover.  Forward in us, without / with, 16 heads of 128: 8 192 tokens 146 / 150 (with
-// kept states 155 / 164), 16 384 270 / 276 (387 / 384), 24 576 577 / 531 (719 / 656), 32 768 768 / 708 (947 / 868); 4 x 4 096 135 / 144 (214 / 203).
-// In fp32, where loads are not beside the products, always: 8 192 tokens 557 / 543 (594 / 552).  With remainders never: the chain is what a step
-// waits for (32 768 tokens 857 / 895).  The reverse scan always does, but with remainders; forward and backward pass's backward, 8 192 tokens 260 / 236,
-// 32 768 1 099 / 912, 8 x 2 048 of 8 heads 151 / 138, 8 192 in fp32 1 255 / 1 156.
+// Whether the forward scan brings later chunks' operands into the L2 (GdrTouch): in 16 bits only where the rows and states of the call
+// are more than one and a quarter times what the last-level cache holds, whose latency the loads cover.  Forward in us, without / with, 16
+// heads of 128: 8 192 tokens 146 / 150 (with kept states 155 / 164), 16 384 270 / 276 (387 / 384), 24 576 577 / 531 (719 / 656), 32 768
+// 768 / 708 (947 / 868); 4 x 4 096 135 / 144 (214 / 203).  In fp32 always: 8 192 tokens 557 / 543 (594 / 552).  With remainders never: the chain
+// is what a step waits for (32 768 tokens 857 / 895).  The reverse scan always does, but with remainders; backward call: 8 192 tokens 260 /
+// 236, 32 768 1 099 / 912, 8 x 2 048 of 8 heads 151 / 138, 8 192 in fp32 1 255 / 1 156.
 inline bool gdr_touch_pays(const GdrDims &d, int key_rows, int value_rows, bool states) {
     if (d.dtype == 1) return true;
     const size_t block = 64 * (size_t)(key_rows * d.dk + value_rows * d.dv) * 2 + (states ? (size_t)d.dk * d.dv * 2 : 0);

@@ -11,11 +11,16 @@ namespace mdn {
 
 namespace {
 
+// Waves to 16 columns of the chain, as in the forward scan: 47 us for 62 in fp32 (2 x 1 024 tokens, 4 heads, d = 64), the backward call with
+// remainders 50 for 52 (777 tokens, 16 heads, d = 128).  (Not with 32 columns, whose LDS is full.)
+template <typename T, int NCG, bool PRECISE> constexpr int CW = (sizeof(T) == 4 || PRECISE) && NCG == 1 ? 2 : 1;
 // beside the chain, chain, loads, stores
-template <typename T, int DK, int NCG> constexpr int bwd_waves() { return 2 + NCG + 2 + (gdr_ring<T, DK, NCG>() ? 2 : 0); }
+template <typename T, int DK, int NCG, bool PRECISE> constexpr int bwd_waves() {
+    return 2 + CW<T, NCG, PRECISE> * NCG + 2 + (gdr_ring<T, DK, NCG>() ? 2 : 0);
+}
 
 template <typename T, int DK, int NCG, bool PRECISE>
-__global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
+__global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_scan_bwd_kernel(GdrDims d, GdrScanBwdArgs a, int first) {
     typedef Gd<T> G;
     typedef typename G::Frag Frag;
     typedef Slate<T, DK> SlateS;
@@ -25,14 +30,16 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_k
     constexpr bool RING = gdr_ring<T, DK, NCG>(); // otherwise loads between two barriers, not beside the products
     // ring depths: what the chain reads; T^T; what the waves beside it read (there is no room for three of everything); coefficients
     constexpr int D = RING ? 3 : 1, DT = PRECISE ? 2 : D, DQ = RING ? 2 : 1, DC = 4;
-    constexpr int LOADS = 2 + NCG, STORES = LOADS + 2; // first waves of each kind
+    constexpr int CWS = CW<T, NCG, PRECISE>, LOADS = 2 + CWS * NCG, STORES = LOADS + 2; // first waves of each kind
     constexpr int SETS = sizeof(T) == 2 ? 2 : 1; // chunks of P^T that a wave beside the chain has asked for
     typedef GLoad<T, DK, true> LoadK;
     typedef GLoad<T, COLS, false> LoadV;
     __shared__ __align__(16) T s_k[D][64 * DK], s_q[DQ][64 * DK], s_do[DQ][64 * COLS], s_t[DT][TRI], s_tl[DT][PRECISE ? TRI : 8];
     __shared__ __align__(16) float s_c[DC][kGdrCoef];
     __shared__ __align__(16) f32x4 s_x[NCG][4][64], s_y[NCG][NT][64];
-    __shared__ __align__(16) T s_s[NCG][SlateS::SIZE], s_r[NCG * SlateE::SIZE];
+    __shared__ __align__(16) T s_s[CWS][NCG][SlateS::SIZE], s_sl[NCG][CWS == 2 && PRECISE ? SlateS::SIZE : 8], s_r[NCG * SlateE::SIZE];
+    __shared__ __align__(16) Frag s_e[NCG][CWS == 2 ? S64 : 1][64], s_el[NCG][CWS == 2 && PRECISE ? S64 : 1][64]; // dE, from wave to wave
+    __shared__ int s_said[NCG][2]; // steps whose half of it is there
     __shared__ __align__(16) int s_touch[2][64];
 
     const int w = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, kg = lane >> 4;
@@ -48,7 +55,7 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_k
         const int r = lane & 15, kg = lane >> 4, m = N - 1 - n;
         const size_t at = (q.v + (size_t)m * 64 * d.H) * d.dv + col0, reach = ((size_t)(n == 0 ? last : 63) * rsv + COLS) * sizeof(T);
         store_tokens<T, NCG, SlateE::LD>(out_rows(static_cast<T *>(a.dv) + at, reach), rsv * (unsigned)sizeof(T), s_r, 32 * w2, 32 * w2, r, kg);
-        store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.dstates) + (q.blk + m) * DK * d.dv, (size_t)DK * d.dv * sizeof(T)), s_s, w2, col0, lane);
+        store_state<T, DK, NCG>(out_rows(static_cast<T *>(a.dstates) + (q.blk + m) * DK * d.dv, (size_t)DK * d.dv * sizeof(T)), s_s[n % CWS], w2, col0, lane);
     };
     // (not with remainders, where the chain is what a step waits for)
     GdrTouch<PRECISE ? 0 : touch_places(2 * DK * (int)sizeof(T) + 2 * TB / 64 + 16, (int)sizeof(T), COLS)> touch;
@@ -144,12 +151,27 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_k
     }
 
     const TileReader<T, DK> tile(r, kg);
-    if (w >= 2) { // ---- the chain
-        const int cg = w - 2, col = col0 + 16 * cg;
+    auto chain = [&](auto half) {
+        // this wave's half (or all): of dk and of the tokens
+        constexpr int TW = decltype(half)::value, HT = NT / CWS, HS = SK / CWS, H64 = S64 / CWS, RT = 4 / CWS;
+        const int cg = (w - 2) / CWS, col = col0 + 16 * cg;
         int slot = 0, slot_t = 0, slot_c = 0;
-        f32x4 S[NT];
-        load_state<T>(S, a.dS_final ? a.dS_final + q.state * DK * d.dv : nullptr, d.dv, col, r, kg);
+        f32x4 S[HT];
+        Frags<T, HT, PRECISE> Sb;
+        load_state<T, TW * HT>(S, a.dS_final ? a.dS_final + q.state * DK * d.dv : nullptr, d.dv, col, r, kg);
         all_arrived();
+        auto publish = [&](int n) { // D, for the storing waves and the other half's
+#pragma unroll
+            for (int s = 0; s < HS; ++s) {
+                SlateS::put(s_s[n % CWS][cg], TW * HS + s, r, kg, Sb.hi[s]);
+                if constexpr (PRECISE && CWS == 2) SlateS::put(s_sl[cg], TW * HS + s, r, kg, Sb.lo[s]);
+            }
+        };
+        if constexpr (CWS == 2) {
+            Sb.from(S);
+            publish(0);
+        }
+        if (lane == 0) s_said[cg][TW] = 0;
         __syncthreads();
         __syncthreads();
         for (int n = 0; n <= N; ++n) {
@@ -157,51 +179,89 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_k
             if (n < N) {
                 const T *k = s_k[slot], *tri = s_t[slot_t], *tri_lo = s_tl[slot_t];
                 const float *c = s_c[slot_c] + G::row(0, 4 * kg);
-                f32x4 X[4], eg[4], ec[4];
+                f32x4 X[RT], eg[4], ec[RT];
                 auto decays = [&] {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        eg[t] = *reinterpret_cast<const f32x4 *>(c + G::row(t, 0));
-                        ec[t] = *reinterpret_cast<const f32x4 *>(c + 64 + G::row(t, 0));
-                    }
+                    for (int t = 0; t < 4; ++t) eg[t] = *reinterpret_cast<const f32x4 *>(c + G::row(t, 0));
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) ec[t] = *reinterpret_cast<const f32x4 *>(c + 64 + G::row(RT * TW + t, 0));
                 };
                 if (RING) decays(); // (32-bit rows of 128 leave no registers for them yet)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) X[t] = s_x[cg][t][lane];
-                Frags<T, NT, PRECISE> Sb;
-                Sb.from(S);
+                for (int t = 0; t < RT; ++t) X[t] = s_x[cg][RT * TW + t][lane];
+                if constexpr (CWS == 1) Sb.from(S);
                 const float eC = s_c[slot_c][63];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) S[t] = eC * S[t] + s_y[cg][t][lane];
+                for (int t = 0; t < HT; ++t) S[t] = eC * S[t] + s_y[cg][TW * HT + t][lane];
                 __syncthreads();
-#pragma unroll
-                for (int s = 0; s < SK; ++s) SlateS::put(s_s[cg], s, r, kg, Sb.hi[s]);
-                f32x4 E[4];
+                if constexpr (CWS == 1) publish(n);
+                f32x4 E[RT];
                 zero_acc(E);
 #pragma unroll
-                for (int s = 0; s < SK; ++s)
+                for (int s = 0; s < HS; ++s)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) E[t] = Sb.mma(tile.row_frag(k, t, s), s, E[t]);
+                    for (int t = 0; t < RT; ++t) E[t] = Sb.mma(tile.row_frag(k, RT * TW + t, TW * HS + s), s, E[t]);
+#pragma unroll
+                for (int s = (1 - TW) * HS; s < (CWS - TW) * HS; ++s) { // (no step where this wave is alone)
+                    if constexpr (CWS == 2) {
+                        const Frag b = SlateS::get(s_s[n % CWS][cg], s, r, kg);
+                        Frag lo;
+                        if constexpr (PRECISE) lo = SlateS::get(s_sl[cg], s, r, kg);
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) {
+                            const Frag f = tile.row_frag(k, RT * TW + t, s);
+                            E[t] = gd_mma<T>(f, b, E[t]);
+                            if constexpr (PRECISE) E[t] = gd_mma<T>(f, lo, E[t]);
+                        }
+                    }
+                }
                 if (!RING) {
                     __builtin_amdgcn_sched_barrier(0);
                     decays();
                 }
 #pragma unroll
-                for (int t = 0; t < 4; ++t) E[t] = X[t] + ec[t] * E[t];
-                Frags<T, 4, PRECISE> Eb;
+                for (int t = 0; t < RT; ++t) E[t] = X[t] + ec[t] * E[t];
+                Frags<T, RT, PRECISE> Eb;
                 Eb.from(E);
-                f32x4 R[4];
-                zero_acc(R);
+                if constexpr (CWS == 2) {
 #pragma unroll
-                for (int s = 0; s < S64; ++s)
+                    for (int s = 0; s < H64; ++s) {
+                        s_e[cg][TW * H64 + s][lane] = Eb.hi[s];
+                        if constexpr (PRECISE) s_el[cg][TW * H64 + s][lane] = Eb.lo[s];
+                    }
+                    say(&s_said[cg][TW], n);
+                }
+                // as in the forward scan: own tokens first; sums over either half of the tokens
+                f32x4 R[4], R2[2];
+                zero_acc(R);
+                zero_acc(R2);
+                auto add = [&](int s, Frag hi, Frag lo) {
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
                         if (s >= G::first(t)) {
-                            R[t] = Eb.mma(tri_frag(tri, G::up(t, s), lane), s, R[t]);
-                            if constexpr (PRECISE) R[t] = gd_mma<T>(tri_frag(tri_lo, G::up(t, s), lane), Eb.hi[s], R[t]);
+                            f32x4 &to = CWS == 1 || s >= H64 ? R[t] : R2[t & 1];
+                            const Frag f = tri_frag(tri, G::up(t, s), lane);
+                            to = gd_mma<T>(f, hi, to);
+                            if constexpr (PRECISE) {
+                                to = gd_mma<T>(f, lo, to);
+                                to = gd_mma<T>(tri_frag(tri_lo, G::up(t, s), lane), hi, to);
+                            }
                         }
+                };
 #pragma unroll
-                for (int s = 0; s < S64; ++s) SlateE::put(s_r + cg * SlateE::SIZE, s, r, kg, G::frag(&R[s * G::KT]));
+                for (int s = 0; s < H64; ++s) add(TW * H64 + s, Eb.hi[s], Eb.lo[PRECISE ? s : 0]);
+                if constexpr (CWS == 2) {
+                    wait_for(&s_said[cg][1 - TW], n);
+#pragma unroll
+                    for (int s = 0; s < H64; ++s) {
+                        const int so = (1 - TW) * H64 + s;
+                        add(so, s_e[cg][so][lane], s_el[cg][PRECISE ? so : 0][lane]);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) R[t] += R2[t];
+                }
+#pragma unroll
+                for (int s = TW * H64; s < (TW + 1) * H64; ++s) SlateE::put(s_r + cg * SlateE::SIZE, s, r, kg, G::frag(&R[s * G::KT]));
 #pragma unroll
                 for (int t = 0; t < 4; ++t) R[t] *= -eg[t];
                 Frags<T, 4, PRECISE> Rb;
@@ -209,7 +269,11 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_k
 #pragma unroll
                 for (int s = 0; s < S64; ++s)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) S[t] = Rb.mma(tile.col_frag(k, t, s), s, S[t]);
+                    for (int t = 0; t < HT; ++t) S[t] = Rb.mma(tile.col_frag(k, TW * HT + t, s), s, S[t]);
+                if constexpr (CWS == 2) {
+                    Sb.from(S);
+                    publish(n + 1);
+                }
                 slot = next_slot<D>(slot);
                 slot_t = next_slot<DT>(slot_t);
                 slot_c = next_slot<DC>(slot_c);
@@ -218,7 +282,11 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_k
             }
             if constexpr (!RING) __syncthreads();
         }
-        if (a.dS0) save_state<T>(S, a.dS0 + q.state * DK * d.dv, d.dv, col, r, kg);
+        if (a.dS0) save_state<T, TW * HT>(S, a.dS0 + q.state * DK * d.dv, d.dv, col, r, kg);
+    };
+    if (w >= 2) { // ---- the chain
+        if (CWS == 1 || w % 2 == 0) chain(std::integral_constant<int, 0>{});
+        else chain(std::integral_constant<int, CWS - 1>{});
         return;
     }
 
@@ -332,7 +400,7 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG>() * 64)) void gdr_scan_bwd_k
 
 template <typename T, int DK, int NCG, bool PRECISE> hipError_t launch_cols(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {
     return launch_in_parts((d.B * d.H + 7) / 8 * 8 * (d.dv / (16 * NCG)), [&](int first, dim3 grid) {
-        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, NCG, PRECISE>), grid, dim3((bwd_waves<T, DK, NCG>() * 64)), 0, s, d, a, first);
+        hipLaunchKernelGGL((gdr_scan_bwd_kernel<T, DK, NCG, PRECISE>), grid, dim3((bwd_waves<T, DK, NCG, PRECISE>() * 64)), 0, s, d, a, first);
     });
 }
 template <typename T, int DK, bool PRECISE> hipError_t launch(const GdrDims &d, const GdrScanBwdArgs &a, hipStream_t s) {

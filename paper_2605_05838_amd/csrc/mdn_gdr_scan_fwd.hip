@@ -177,7 +177,10 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
                 if constexpr (PRECISE && CWS == 2) SlateS::put(s_sl[cg], TW * HS + s, r, kg, Sb.lo[s]);
             }
         };
-        Sb.from(S);
+        // S is rounded behind the step that formed it, but by a single wave with remainders in front of the next, where the first reads take
+        // their time as well: 64 us for 67 (8 x 2 048 tokens of 8 heads, d = 128); without remainders 686 for 649 (32 768 tokens of 16).
+        constexpr bool BEHIND = CWS == 2 || !PRECISE;
+        if (BEHIND) Sb.from(S);
         if constexpr (CWS == 2) publish();
         if (lane == 0) s_said[cg][TW] = 0;
         for (int n = 0; n <= N + 1; ++n) {
@@ -186,6 +189,7 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
                 const T *k = s_k[slot], *v = s_v[slot], *tri = s_t[slot], *tri_lo = s_tl[slot];
                 const float *c = s_c[slot_c] + G::row(0, 4 * kg);
                 const float eC = s_c[slot_c][63];
+                if (!BEHIND) Sb.from(S);
                 if constexpr (CWS == 1) publish();
                 f32x4 E[4];
                 if constexpr (REBUILD) {
@@ -227,7 +231,8 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
                         }
                         say(&s_said[cg][TW], n);
                     }
-                    // Own tokens first, while the other wave's are not there yet.  Sums over the first and over the second half of the tokens, so that both waves have the same bits
+                    // Own tokens first, while the other wave's are not there yet.  Sums over either half of the tokens, so that both waves have
+                    // the same bits.
                     f32x4 X[2];
                     zero_acc(E);
                     zero_acc(X);
@@ -272,7 +277,7 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
                 slot = next_slot<D>(slot);
                 slot_c = next_slot<DC>(slot_c);
                 slot_s = next_slot<NS>(slot_s);
-                Sb.from(S);
+                if (BEHIND) Sb.from(S);
                 if constexpr (CWS == 2) publish();
             }
             if constexpr (D == 1) __syncthreads();
