@@ -215,7 +215,9 @@ int mdn_recurrent_step(const mdn_shape *shape, const void *q, const void *k, con
  * With 16-bit storage the products take bf16 operands and sum in fp32.  A state that leaves the call in 32 bits (S_final, dS0) is carried with
  * operands of twice the bits (value + remainder) and is good to about 2^-17; ask for it only where it is wanted.  States the backward keeps
  * for itself are rounded to the storage dtype.  All pointers 16-byte aligned.  Results do not depend on anything but the arguments:
- * repeated calls agree bit for bit.  No call synchronises or allocates; launches are not recorded by the timing facility below.
+ * repeated calls agree bit for bit.  No call synchronises or allocates device memory; launches are not recorded by the timing facility below.
+ * A long backward call with few heads is split over the library's second stream, as mdn_chunk_bwd is, and joined back into `stream`.
+ * No tensor that a call writes may overlap another of its tensors, but where it is said below.
  */
 typedef struct mdn_gdr_shape {
     int32_t B, T, H, Hk; /* batch, sequence length, value heads, key heads */
@@ -363,7 +365,7 @@ int mdn_profile_begin_sampled(int period);
 int mdn_profile_launch_counts(int *launched, int n);
 
 /*
- * Number of segments mdn_chunk_fwd / mdn_chunk_bwd split the sequence into: k >= 1 forces k
+ * Number of segments mdn_chunk_fwd / mdn_chunk_bwd / mdn_gdr_chunk_bwd split the sequence into: k >= 1 forces k
  * (1 = never split; capped at N/4 and at 16), 0 restores the automatic choice.  A tuning and
  * test knob: results do not depend on it (states cross a segment boundary in fp32, exactly as
  * they are carried inside a scan).  Returns the previous setting (an atomic exchange: process-wide).

@@ -228,7 +228,7 @@ def mdn_recurrent_step(q, k, v, beta, alpha, mu, S, M, eta=None, scale=None, out
 
 
 def set_segments(k):
-    """Force the number of sequence segments of mdn_chunk_fwd / mdn_chunk_bwd (0 = automatic); returns the old value."""
+    """Force the number of sequence segments of mdn_chunk_fwd / mdn_chunk_bwd / mdn_gdr_chunk_bwd (0 = automatic); returns the old value."""
     return int(load_library().mdn_set_segments(int(k)))
 
 

@@ -2,6 +2,7 @@
 // Declarations and the contract of every entry point are in include/mdn.h.
 #include "../../include/mdn.h"
 #include "mdn_kernels.h"
+#include "mdn_side.h"
 
 #include <hip/hip_runtime.h>
 #include <string.h>
@@ -168,6 +169,40 @@ template <typename F> int timed(int id, hipStream_t s, F &&launch) {
 // chunk-local kernel takes a twentieth to a seventh of the scan's time, less than the boundaries cost.
 std::atomic<int> g_segments{0}; // 0: automatic
 
+} // namespace
+
+namespace mdn {
+
+int requested_segments() { return g_segments.load(std::memory_order_relaxed); }
+
+Side *side_device() {
+    static Side per_device[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return nullptr;
+    return &per_device[dev];
+}
+Side *side(int n) {
+    Side *xp = side_device();
+    if (!xp) return nullptr;
+    Side &x = *xp;
+    if (!x.stream && hipStreamCreateWithFlags(&x.stream, hipStreamNonBlocking) != hipSuccess) return nullptr;
+    try {
+        x.ev.reserve(n);
+    } catch (const std::bad_alloc &) {
+        return nullptr;
+    }
+    while ((int)x.ev.size() < n) {
+        hipEvent_t e;
+        if (hipEventCreateWithFlags(&e, hipEventDisableTiming) != hipSuccess) return nullptr;
+        x.ev.push_back(e);
+    }
+    return &x;
+}
+
+} // namespace mdn
+
+namespace {
+
 // the serial scans of a call would occupy at most half of the CUs
 bool few_scan_workgroups(const Dims &d) { return 2 * scan_workgroups(d) <= num_cus(); }
 
@@ -194,45 +229,10 @@ long long backward_segments(const Dims &d, bool rebuild) {
 }
 int segments(const Dims &d, bool backward, bool rebuild = false) {
     if (t_no_alloc || d.packed) return 1; // (packed batches: the scans of the sequences run beside each other)
-    long long k = g_segments.load(std::memory_order_relaxed);
+    long long k = requested_segments();
     if (k <= 0) k = backward ? backward_segments(d, rebuild) : 1;
     k = std::min(k, (long long)d.N / 4);
     return (int)std::max(1LL, std::min(16LL, k));
-}
-
-// The library's second stream and its events, one set per device, shared by every call on that device.  A call that
-// uses them holds the device's mutex while it ENQUEUES (the kernels themselves run after it has returned): an event
-// is recorded and waited for inside one such section, so calls from several host threads cannot interleave their
-// record / wait pairs; their work on the second stream is simply ordered one call after the other.
-struct Side {
-    hipStream_t stream = nullptr;
-    std::vector<hipEvent_t> ev;
-    std::mutex mutex;
-};
-
-// the second stream and n events on the current device (created once, default priority); call with the lock held
-Side *side_device() {
-    static Side per_device[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return nullptr;
-    return &per_device[dev];
-}
-Side *side(int n) {
-    Side *xp = side_device();
-    if (!xp) return nullptr;
-    Side &x = *xp;
-    if (!x.stream && hipStreamCreateWithFlags(&x.stream, hipStreamNonBlocking) != hipSuccess) return nullptr;
-    try {
-        x.ev.reserve(n);
-    } catch (const std::bad_alloc &) {
-        return nullptr;
-    }
-    while ((int)x.ev.size() < n) {
-        hipEvent_t e;
-        if (hipEventCreateWithFlags(&e, hipEventDisableTiming) != hipSuccess) return nullptr;
-        x.ev.push_back(e);
-    }
-    return &x;
 }
 
 Dims segment(const Dims &d, int i, int k) {

@@ -21,6 +21,7 @@ namespace mdn {
 struct GdrDims {
     int B, T, H, Hk;   // B sequences of T tokens; packed batches: B sequences of their own lengths, T tokens together
     int N, nchunks;    // chunks of the longest sequence, of all sequences
+    int c0, cn;        // sequences of equal lengths: a launch's chunks of each, [c0, c0 + cn) of the N
     int dk, dv, dtype; // MDN_DTYPE_*
     float scale;
     const SeqEntry *seqs;     // packed batches: [B], longest first; otherwise null
@@ -102,6 +103,7 @@ template <> struct Gd<bf16_t> {
     }
     // what frag() dropped
     static __device__ __forceinline__ Frag rest(const f32x4 *c, Frag f) {
+#pragma clang fp contract(off) // (of the value as it was rounded to 32 bits, wherever the compiler inlines this: results do not depend on it)
         Frag r;
 #pragma unroll
         for (int e = 0; e < 8; ++e) r[e] = (bf16_t)(c[e >> 2][e & 3] - (float)f[e]);
@@ -247,11 +249,12 @@ __device__ __forceinline__ GdrSeq gdr_seq(const GdrDims &d, int bh) {
         q.blk = (size_t)e.cb * d.H + (size_t)h * q.n;
         q.state = (size_t)e.idx * d.H + h;
     } else {
-        q.n = d.N;
-        q.len = d.T;
-        q.v = (size_t)b * d.T * d.H + h;
-        q.k = (size_t)b * d.T * d.Hk + hk;
-        q.blk = (size_t)bh * d.N;
+        const size_t t0 = (size_t)b * d.T + (size_t)d.c0 * 64;
+        q.n = d.cn;
+        q.len = min(d.T - d.c0 * 64, d.cn * 64);
+        q.v = t0 * d.H + h;
+        q.k = t0 * d.Hk + hk;
+        q.blk = (size_t)bh * d.N + d.c0;
         q.state = bh;
     }
     return q;
@@ -269,7 +272,7 @@ __device__ __forceinline__ GdrChunk gdr_chunk(const GdrDims &d, int c, int h) {
         p.blk = (size_t)e.blk + (size_t)h * e.N;
         p.rows = e.rows;
     } else {
-        const int b = c / d.N, n = c % d.N;
+        const int b = c / d.cn, n = d.c0 + c % d.cn;
         p.tok = (size_t)b * d.T + (size_t)n * 64;
         p.blk = ((size_t)b * d.H + h) * d.N + n;
         p.rows = min(64, d.T - n * 64);

@@ -1,9 +1,11 @@
 // C ABI of the gated delta rule: argument checks, workspace carving, kernel sequencing.  The contract is in include/mdn.h.
 #include "../../include/mdn.h"
 #include "mdn_gdr.h"
+#include "mdn_side.h"
 
 #include <hip/hip_runtime.h>
 #include <algorithm>
+#include <mutex>
 #include <new>
 #include <vector>
 
@@ -31,6 +33,7 @@ int check_shape(const mdn_gdr_shape *s, GdrDims *d) {
     *d = GdrDims{};
     d->B = s->B; d->T = s->T; d->H = s->H; d->Hk = s->Hk;
     d->N = (int)(((long long)s->T + 63) / 64);
+    d->cn = d->N;
     d->nchunks = (int)((long long)s->B * d->N);
     d->dk = s->dk; d->dv = s->dv; d->dtype = s->dtype; d->scale = s->scale;
     return MDN_OK;
@@ -123,7 +126,7 @@ Operands carve_operands(const GdrDims &d, void *p) {
     return w;
 }
 
-struct BwdWs { Tables tables; Operands op; void *TT_lo, *PT_lo, *states, *dstates, *sums; size_t total; };
+struct BwdWs { Tables tables; Operands op; void *TT_lo, *PT_lo, *states, *dstates, *sums; float *carry; size_t total; };
 BwdWs carve_bwd(const GdrDims &d, bool packed, void *ws) {
     Carve c(ws);
     BwdWs w;
@@ -136,8 +139,41 @@ BwdWs carve_bwd(const GdrDims &d, bool packed, void *ws) {
     w.states = c.take(states_bytes(d));
     w.dstates = c.take(states_bytes(d));
     w.sums = d.H > d.Hk ? c.take((size_t)d.nchunks * d.Hk * gdr_sums_bytes(d.dk)) : nullptr;
+    w.carry = packed ? nullptr : c.take<float>((size_t)d.B * d.H * d.dk * d.dv * sizeof(float));
     w.total = c.off;
     return w;
+}
+
+// Segments of a backward call: with scan workgroups for at most half of the CUs, the gradient launch of one runs beside the reverse scan of the
+// one before it (in time) on the library's second stream, and so does the states' reconstruction beside the first scans.  The adjoint crosses
+// a boundary in 32 bits, as the scan carries it: results do not depend on the number.  (Packed sequences' scans run beside each other.)
+// A boundary costs ~10 us and hides a gradient launch, 40 us per 1 024 chunk blocks of d = 128: a segment per 1 024, at most 4; where the states are
+// reconstructed, which the gradient launches wait for, 2, but with remainders, whose scans take longer, as many.  Backward in us, 1 / 2 / 4 / 8
+// segments, states kept; reconstructed; reconstructed, with dS0 (16 heads of 128 unless said):
+//    4 096 tokens    123 /   135 /   147 /   185;     171 /   149 /   171 /   231;     212 /   213 /   220 /   233
+//    8 192           234 /   231 /   230 /   263;     328 /   255 /   269 /   315;     417 /   386 /   369 /   403
+//   16 384           466 /   427 /   409 /   439;     676 /   503 /   524 /   555;     868 /   740 /   707 /   722
+//   32 768           912 /   804 /   749 /   758;   1 355 /   952 /   983 / 1 032;   1 769 / 1 449 / 1 345 / 1 372
+//   32 768, 4 heads  681 /   668 /   673 /   708;     967 /   697 /   691 /   725;   1 297 / 1 066 / 1 054 / 1 077
+//   65 536, d = 64 1 341 / 1 261 / 1 240 / 1 250;   2 019 / 1 582 / 1 559 / 1 615;   2 602 / 2 039 / 1 946 / 1 980
+//    4 096, 8, fp32  366 /   351 /   374 /   443;     501 /   374 /   395 /   555
+int segments(const GdrDims &d, bool rebuild, bool precise) {
+    if (d.seqs) return 1;
+    long long k = requested_segments();
+    if (k <= 0) {
+        if (2LL * ((d.B * d.H + 7) / 8 * 8) * (d.dv / 16) > num_cus()) return 1;
+        k = (long long)d.nchunks * d.H * d.dk * (d.dtype == MDN_DTYPE_F32 ? 4 : 1) / (128 * 1024);
+        if (rebuild && !precise && k) k = 2;
+        k = std::min({4LL, d.N / 32LL, k});
+    }
+    return (int)std::max(1LL, std::min({16LL, k, d.N / 4LL}));
+}
+GdrDims segment(const GdrDims &d, int i, int k) {
+    GdrDims r = d;
+    r.c0 = (int)((long long)d.N * i / k);
+    r.cn = (int)((long long)d.N * (i + 1) / k) - r.c0;
+    r.nchunks = d.B * r.cn;
+    return r;
 }
 
 int status(hipError_t e) { return e == hipSuccess ? MDN_OK : MDN_ERR_LAUNCH; }
@@ -227,24 +263,54 @@ int mdn_gdr_chunk_bwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int
         rc = status(launch_gdr_local(d, l, s));
         if (rc) return rc;
     }
-    const void *states = states_saved;
-    if (!states) { // before anything is written over S0
-        GdrScanFwdArgs a = {};
-        a.k = k; a.v = e_saved; a.coef = op.coef; a.S0 = S0; a.states = w.states;
-        rc = status(launch_gdr_rebuild(d, a, s));
-        if (rc) return rc;
-        states = w.states;
-    }
+    GdrScanFwdArgs a = {}; // the states' reconstruction, where they were not kept
+    a.k = k; a.v = e_saved; a.coef = op.coef; a.S0 = S0; a.states = w.states;
     GdrScanBwdArgs b = {};
     b.q = q; b.k = k; b.dO = dO; b.coef = op.coef; b.TT = op.TT; b.PT = op.PT;
     if (precise) b.TT_lo = w.TT_lo, b.PT_lo = w.PT_lo;
     b.dS_final = dS_final; b.dv = dv; b.dstates = w.dstates; b.dS0 = dS0;
-    rc = status(launch_gdr_scan_bwd(d, b, precise, s));
-    if (rc) return rc;
     GdrGradArgs c = {};
-    c.q = q; c.k = k; c.e = e_saved; c.dO = dO; c.dv = dv; c.g = g; c.beta = beta; c.states = states; c.dstates = w.dstates;
-    c.sums = w.sums; c.dq = dq; c.dk = dk; c.dg = dg; c.dbeta = dbeta;
-    return status(launch_gdr_grad(d, c, s));
+    c.q = q; c.k = k; c.e = e_saved; c.dO = dO; c.dv = dv; c.g = g; c.beta = beta; c.states = states_saved ? states_saved : w.states;
+    c.dstates = w.dstates; c.sums = w.sums; c.dq = dq; c.dk = dk; c.dg = dg; c.dbeta = dbeta;
+    const int nseg = segments(d, !states_saved, precise);
+    if (nseg == 1) {
+        if (!states_saved) { // before anything is written over S0
+            rc = status(launch_gdr_rebuild(d, a, s));
+            if (rc) return rc;
+        }
+        rc = status(launch_gdr_scan_bwd(d, b, precise, s));
+        if (rc) return rc;
+        return status(launch_gdr_grad(d, c, s));
+    }
+    Side *sdev = side_device();
+    if (!sdev) return MDN_ERR_LAUNCH;
+    std::lock_guard<std::mutex> lock(sdev->mutex);
+    Side *sd = side(nseg + 3);
+    if (!sd) return MDN_ERR_LAUNCH;
+    auto hand_over = [&](hipEvent_t e, hipStream_t from, hipStream_t to) {
+        return hipEventRecord(e, from) == hipSuccess && hipStreamWaitEvent(to, e, 0) == hipSuccess ? MDN_OK : MDN_ERR_LAUNCH;
+    };
+    if (!states_saved) {
+        rc = hand_over(sd->ev[nseg], s, sd->stream);
+        if (rc) return rc;
+        rc = status(launch_gdr_rebuild(d, a, sd->stream));
+        if (hipEventRecord(sd->ev[nseg + 1], sd->stream) != hipSuccess) rc = MDN_ERR_LAUNCH;
+    }
+    for (int i = nseg - 1; i >= 0 && !rc; --i) { // the last one first
+        const GdrDims di = segment(d, i, nseg);
+        b.dS_final = i == nseg - 1 ? dS_final : w.carry;
+        b.dS0 = i == 0 ? dS0 : w.carry;
+        if (i == 0 && dS0 && !states_saved) { // it may be written over S0, which the reconstruction reads
+            if (hipStreamWaitEvent(s, sd->ev[nseg + 1], 0) != hipSuccess) rc = MDN_ERR_LAUNCH;
+            if (rc) break;
+        }
+        rc = status(launch_gdr_scan_bwd(di, b, precise, s));
+        if (!rc) rc = hand_over(sd->ev[i], s, sd->stream);
+        if (!rc) rc = status(launch_gdr_grad(di, c, sd->stream));
+    }
+    // the caller's stream waits for whatever went to the second stream, also when a launch failed on the way
+    const int joined = hand_over(sd->ev[nseg + 2], sd->stream, s);
+    return rc ? rc : joined;
 }
 
 int mdn_gdr_recurrent_step(const mdn_gdr_shape *shape, const void *q, const void *k, const void *v, const float *g, const float *beta,
