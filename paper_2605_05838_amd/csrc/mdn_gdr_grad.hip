@@ -40,6 +40,7 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
     typedef GTile<T, 64> TileV;
     constexpr int E = G::E, S64 = 64 / G::KS, SK = DK / G::KS, NP = DK / 32; // NP: 32-row parts of dk
     constexpr int NI = NP, I0 = 4 / NI; // token tiles of a wave (DK = 128: all four); waves that share a part
+    constexpr int EARLY = sizeof(T) == 4 ? 0 : SHARED && DK + DV == 256 ? 1 : 2; // steps whose state fragments are asked for early (registers)
     static_assert(NI * I0 == 4 && (DK == 64 || DK == 128) && (DV == 64 || DV == 128), "sizes");
     __shared__ __align__(16) T s_k[64 * DK], s_q[64 * DK];
     __shared__ __align__(16) T s_e[64 * 64], s_do[64 * 64], s_dv[64 * 64]; // halves of E, dO, dV
@@ -101,21 +102,22 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
             for (int u = 0; u < 2; ++u) dq[i][u] = dk[i][u] = wk[i][u] = f32x4{0.f, 0.f, 0.f, 0.f};
         const unsigned pairs = kPairs[w];
         float trace = 0.f;
+        auto fragments = [&](Frag &sf, Frag &df, int hv, int s, int u) {
+            const size_t at = (size_t)((hv * S64 + s) * (DK / 16) + u) * 64;
+            sf = Sg[at];
+            df = Dg[at];
+        };
         auto states = [&](Frag (&sf)[S64][2], Frag (&df)[S64][2], int hv) {
 #pragma unroll
-            for (int s = 0; s < S64; ++s)
+            for (int s = 0; s < EARLY; ++s)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const size_t at = (size_t)((hv * S64 + s) * (DK / 16) + u) * 64;
-                    sf[s][u] = Sg[at];
-                    df[s][u] = Dg[at];
-                }
+                for (int u = 0; u < 2; ++u) fragments(sf[s][u], df[s][u], hv, s, u);
         };
 #pragma unroll 1
         for (int hv = 0; hv < DV / 64; ++hv) {
             // In 16 bits asked for before the tiles, so that one wait covers both: 183 us for 200, [4, 4 096] tokens, 16 heads, d = 128
             Frag sf[S64][2], df[S64][2];
-            if constexpr (sizeof(T) == 2) states(sf, df, hv);
+            states(sf, df, hv);
             if (hv) __syncthreads(); // the tiles before these are done with
             tile(TileV{}, s_e, static_cast<const T *>(a.e) + val + hv * 64, rsv);
             tile(TileV{}, s_do, static_cast<const T *>(a.dO) + val + hv * 64, rsv);
@@ -141,11 +143,7 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
             for (int s = 0; s < S64; ++s)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    if constexpr (sizeof(T) == 4) {
-                        const size_t at = (size_t)((hv * S64 + s) * (DK / 16) + u) * 64;
-                        sf[s][u] = Sg[at];
-                        df[s][u] = Dg[at];
-                    }
+                    if (s >= EARLY) fragments(sf[s][u], df[s][u], hv, s, u);
                     if (it0 == 0) trace += dot(sf[s][u], df[s][u]); // (once per part)
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll

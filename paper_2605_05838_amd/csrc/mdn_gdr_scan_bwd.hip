@@ -215,9 +215,10 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
                         }
                     }
                 }
-                if (!RING) {
+                if (!RING) { // (fenced in: phases mixed by the compiler need more registers than there are)
                     __builtin_amdgcn_sched_barrier(0);
                     decays();
+                    __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
                 for (int t = 0; t < RT; ++t) E[t] = X[t] + ec[t] * E[t];
