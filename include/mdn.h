@@ -217,6 +217,7 @@ int mdn_recurrent_step(const mdn_shape *shape, const void *q, const void *k, con
  * for itself are rounded to the storage dtype.  All pointers 16-byte aligned.  Results do not depend on anything but the arguments:
  * repeated calls agree bit for bit.  No call synchronises or allocates device memory; launches are not recorded by the timing facility below.
  * A long backward call with few heads is split over the library's second stream, as mdn_chunk_bwd is, and joined back into `stream`.
+ * (Captured, it takes that stream into the capture: no other call that is split, on the same device, until the capture has ended.)
  * No tensor that a call writes may overlap another of its tensors, but where it is said below.
  */
 typedef struct mdn_gdr_shape {
