@@ -82,7 +82,7 @@ hipError_t launch_gdr_step(const GdrDims &d, const GdrStepArgs &a, hipStream_t s
 inline size_t gdr_triangle_bytes(int dtype) { return dtype == 1 ? 10240 : 6144; }
 
 // 32-bit sums of dq, dk and two triangles over the value heads of a key head, per chunk and key head
-inline size_t gdr_sums_bytes(int dk) { return (size_t)(2 * 64 * dk + 2 * 3072) * sizeof(float); }
+inline size_t gdr_sums_bytes(int dk) { return (size_t)(2 * 64 * dk + 2 * 12 * 256) * sizeof(float); }
 
 // ---- layouts
 template <typename T> struct Gd;
