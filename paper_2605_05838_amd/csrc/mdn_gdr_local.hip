@@ -3,7 +3,8 @@
 // One workgroup of four waves per (chunk, value head).  The ten 16x16 tiles on and below the diagonal of K K^T and Q K^T are dealt
 // to the waves in pairs that share a B fragment; the inverse is fp32 whatever the storage.  T, P and their transposes leave as the
 // fragments that the scans load (mdn_gdr.h), triangles only: 6 KB each of 16-bit storage.  The K and Q tiles, dead after the
-// products, make room for A and P: 37 KB of LDS, four workgroups per CU.
+// products, make room for A and P: 37 KB of LDS, four workgroups per CU.  Bound by HBM: 4 x 4 096 tokens of 16 heads of 128, all four
+// triangles written, 54 us for 230 MB, 4.3 TB/s.
 #include "mdn_coef.h"
 #include "mdn_gdr.h"
 

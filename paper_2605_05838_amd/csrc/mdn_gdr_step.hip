@@ -1,6 +1,6 @@
 // Gated delta rule, token by token (decoding):
 //     S <- e^{g} S;   e = v - S^T k;   S <- S + beta k e^T;   o = scale S^T q
-// Bound by reading and writing the fp32 state once per call.  A workgroup owns COLS columns of one (sequence, value head); a thread has
+// Bound by reading and writing the fp32 state once per call (256 sequences of 16 heads of 128 among other work: 100 us, 5.4 TB/s; one: 2.9).  A workgroup owns COLS columns of one (sequence, value head); a thread has
 // dk COLS / 1024 rows of 4 neighbouring columns in registers, so that a wave moves whole 128-byte lines; the two sums over dk go over the
 // lanes of a wave, then over the four waves through LDS.  A token's operands are requested one token ahead.
 #include "mdn_gdr.h"
@@ -89,9 +89,12 @@ template <typename T, int DK, int COLS, bool NT> hipError_t launch_cols(const Gd
         hipLaunchKernelGGL((gdr_step_kernel<T, DK, COLS, NT>), grid, dim3(kThreads), 0, s, d, a, first);
     });
 }
+// 32 columns where workgroups of 64 would leave half of the CUs without one: calls on the same states in us, 32 / 64 columns, 1 sequence of 16
+// heads of 128 2.9 / 3.2, 8 4.5 / 4.5, 24 8.1 / 7.6, 256 79 / 76; 12 x 5 tokens, 8 heads of 64 x 128 in fp32 6.6 / 6.3.  States past what the
+// last-level cache gives back to the next call go by it, plain / non-temporal: 256 sequences 76 / 90, 300 95 / 107, 360 130 / 128, 512 201 / 184.
 template <typename T, int DK> hipError_t launch_t(const GdrDims &d, const GdrStepArgs &a, hipStream_t s) {
     const long long bytes = 4LL * d.B * d.H * DK * d.dv;
-    if ((long long)d.B * d.H * (d.dv / 64) < 4LL * num_cus()) return launch_cols<T, DK, 32, false>(d, a, s);
+    if (2LL * d.B * d.H * (d.dv / 64) < num_cus()) return launch_cols<T, DK, 32, false>(d, a, s);
     if (bytes <= (352LL << 20)) return launch_cols<T, DK, 64, false>(d, a, s);
     return launch_cols<T, DK, 64, true>(d, a, s);
 }
