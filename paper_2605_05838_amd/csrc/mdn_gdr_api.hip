@@ -150,13 +150,13 @@ BwdWs carve_bwd(const GdrDims &d, bool packed, void *ws) {
 // A boundary costs ~10 us and hides a gradient launch, 40 us per 1 024 chunk blocks of d = 128: a segment per 1 024, at most 4; where the states are
 // reconstructed, which the gradient launches wait for, 2, but with remainders, whose scans take longer, as many.  Backward in us, 1 / 2 / 4 / 8
 // segments, states kept; reconstructed; reconstructed, with dS0 (16 heads of 128 unless said):
-//    4 096 tokens    123 /   135 /   147 /   185;     171 /   149 /   171 /   231;     212 /   213 /   220 /   233
-//    8 192           234 /   231 /   230 /   263;     328 /   255 /   269 /   315;     417 /   386 /   369 /   403
-//   16 384           466 /   427 /   409 /   439;     676 /   503 /   524 /   555;     868 /   740 /   707 /   722
-//   32 768           912 /   804 /   749 /   758;   1 355 /   952 /   983 / 1 032;   1 769 / 1 449 / 1 345 / 1 372
-//   32 768, 4 heads  681 /   668 /   673 /   708;     967 /   697 /   691 /   725;   1 297 / 1 066 / 1 054 / 1 077
-//   65 536, d = 64 1 341 / 1 261 / 1 240 / 1 250;   2 019 / 1 582 / 1 559 / 1 615;   2 602 / 2 039 / 1 946 / 1 980
-//    4 096, 8, fp32  366 /   351 /   374 /   443;     501 /   374 /   395 /   555
+//    4 096 tokens    117 /   128 /   142 /   182;     170 /   149 /   173 /   230;     211 /   212 /   220 /   233
+//    8 192           231 /   228 /   228 /   261;     330 /   260 /   277 /   321;     418 /   388 /   371 /   404
+//   16 384           465 /   425 /   404 /   430;     677 /   499 /   522 /   558;     867 /   741 /   706 /   721
+//   32 768           915 /   810 /   761 /   761;   1 349 /   948 /   984 / 1 032;   1 767 / 1 441 / 1 341 / 1 337
+//   32 768, 4 heads  672 /   665 /   668 /   704;     960 /   693 /   685 /   731;   1 287 / 1 060 / 1 050 / 1 082
+//   65 536, d = 64 1 332 / 1 260 / 1 227 / 1 247;   2 019 / 1 585 / 1 560 / 1 608;   2 594 / 2 035 / 1 946 / 1 962
+//    4 096, 8, fp32  361 /   348 /   372 /   441;     497 /   374 /   394 /   556;     498 /   421 /   397 /   556
 int segments(const GdrDims &d, bool rebuild, bool precise) {
     if (d.seqs) return 1;
     long long k = requested_segments();

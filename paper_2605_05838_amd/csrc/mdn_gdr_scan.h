@@ -226,8 +226,8 @@ template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void save_s
 // are more than one and a quarter times what the last-level cache holds, whose latency the loads cover.  Forward in us, without / with, 16
 // heads of 128: 8 192 tokens 146 / 150 (with kept states 155 / 164), 16 384 270 / 276 (387 / 384), 24 576 577 / 531 (719 / 656), 32 768
 // 768 / 708 (947 / 868); 4 x 4 096 135 / 144 (214 / 203).  In fp32 always: 8 192 tokens 557 / 543 (594 / 552).  With remainders never: the chain
-// is what a step waits for (32 768 tokens 857 / 895).  The reverse scan always does, but with remainders; backward call: 8 192 tokens 260 /
-// 236, 32 768 1 099 / 912, 8 x 2 048 of 8 heads 151 / 138, 8 192 in fp32 1 255 / 1 156.
+// is what a step waits for (32 768 tokens 857 / 895).  The reverse scan always does, but with remainders; backward call: 8 192 tokens 254 /
+// 231, 32 768 1 064 / 912, 8 x 2 048 of 8 heads 145 / 139, 777 33.6 / 33.2, 8 192 in fp32 1 020 / 916, [2, 1 024] of 4 heads of 64 67.4 / 67.7.
 inline bool gdr_touch_pays(const GdrDims &d, int key_rows, int value_rows, bool states) {
     if (d.dtype == 1) return true;
     const size_t block = 64 * (size_t)(key_rows * d.dk + value_rows * d.dv) * 2 + (states ? (size_t)d.dk * d.dv * 2 : 0);
@@ -235,9 +235,9 @@ inline bool gdr_touch_pays(const GdrDims &d, int key_rows, int value_rows, bool 
 }
 
 // 16 columns per workgroup while there is a CU for each of these workgroups, or 32.  Calls in us, 16 / 32 columns, heads of 128: forward with
-// kept states, with final states, backward: 777 tokens of 16 heads 24.5 / 25.3, 28.9 / 33.3, 34.0 / 36.8; 2 x 2 048 (256 workgroups of 16 columns)
-// 55.2 / 55.7, 67 / 75, 88 / 90; 3 x 2 048 (384) 93 / 65, 114 / 83, 142 / 109; 8 x 2 048 262 / 200, 239 / 165, 345 / 283; heads of 64, where two
-// would share a CU, 8 x 2 048 (512) 109 / 87, 113 / 85, 147 / 134.
+// kept states, with final states, backward, with adjoints of the initial states: 777 tokens of 16 heads 24.5 / 25.3, 28.9 / 33.3, 33.2 / 35.8, 49 / 54;
+// 2 x 2 048 (256 workgroups of 16 columns) 55.2 / 55.7, 67 / 75, 83 / 88, 120 / 128; 3 x 2 048 (384) 93 / 65, 114 / 83, 141 / 107, 206 / 157;
+// 8 x 2 048 262 / 200, 239 / 165, 338 / 277, 479 / 384; heads of 64, where two would share a CU, 8 x 2 048 (512) 109 / 87, 113 / 85, 149 / 135, 223 / 184.
 inline bool gdr_one_group(const GdrDims &d) { return (long long)(d.B * d.H + 7) / 8 * 8 * (d.dv / 16) <= num_cus(); }
 
 } // namespace mdn

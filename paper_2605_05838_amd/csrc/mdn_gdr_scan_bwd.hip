@@ -5,14 +5,16 @@
 // Two barriers a step: at its start, and when the chain has taken X and Y and the storing waves have taken the step before's D and dV:
 // then either side writes the next.
 // PRECISE (a call that asks for dS0, which is 32-bit): as in the forward scan; P^T and e^G dO' have remainders as well (dO and Q are exact).
+#include "mdn_gdr_ring.h"
 #include "mdn_gdr_scan.h"
 
 namespace mdn {
 
 namespace {
 
-// Waves to 16 columns of the chain, as in the forward scan: 47 us for 62 in fp32 (2 x 1 024 tokens, 4 heads, d = 64), the backward call with
-// remainders 50 for 52 (777 tokens, 16 heads, d = 128).  (Not with 32 columns, whose LDS is full.)
+// Waves to 16 columns of the chain, as in the forward scan, two for one, backward calls: 68 us for 84 in fp32 (2 x 1 024 tokens, 4 heads, d = 64),
+// 916 for 1 221 (8 192 of 16, d = 128), with remainders 49 for 52 (777 tokens, 16 heads, d = 128), 1 366 for 1 449 (32 768).  (Not with 32
+// columns, whose LDS is full.)
 template <typename T, int NCG, bool PRECISE> constexpr int CW = (sizeof(T) == 4 || PRECISE) && NCG == 1 ? 2 : 1;
 // beside the chain, chain, loads, stores
 template <typename T, int DK, int NCG, bool PRECISE> constexpr int bwd_waves() {
@@ -29,7 +31,7 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
     constexpr int TB = TRI * (int)sizeof(T); // bytes of a triangle
     constexpr bool RING = gdr_ring<T, DK, NCG>(); // otherwise loads between two barriers, not beside the products
     // ring depths: what the chain reads; T^T; what the waves beside it read (there is no room for three of everything); coefficients
-    constexpr int D = RING ? 3 : 1, DT = PRECISE ? 2 : D, DQ = RING ? 2 : 1, DC = 4;
+    constexpr int D = RING ? kReverseK : 1, DT = RING ? reverse_t(PRECISE) : 1, DQ = RING ? kReverseQ : 1, DC = kReverseCoef;
     constexpr int CWS = CW<T, NCG, PRECISE>, LOADS = 2 + CWS * NCG, STORES = LOADS + 2; // first waves of each kind
     constexpr int SETS = sizeof(T) == 2 ? 2 : 1; // chunks of P^T that a wave beside the chain has asked for
     typedef GLoad<T, DK, true> LoadK;
@@ -105,34 +107,17 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
             (n == 0 ? lk_end : lk).request(qq + (size_t)m * 64 * rsk, s_q[n % DQ], w2);
             (n == 0 ? lv_end : lv).request(v + (size_t)m * 64 * rsv, s_do[n % DQ], w2);
         };
-        get_q(0);
-        wait_vm<0>();
-        __syncthreads();
-        if constexpr (!RING) aim_touch(w2);
         if constexpr (RING) {
-            get_k(0);
-            get_t(0);
-            if (N > 1) {
-                get_q(1);
-                get_k(1);
-                if (DT == D) get_t(1);
-            }
+            // (requests of K and T^T by either wave)
+            constexpr int LAST = LoadK::COUNT + (DT == D ? TB / 2048 : 0);
+            reverse_ring<DT>(N, get_q, get_k, get_t, [](bool all) { all ? wait_vm<0>() : wait_vm<LAST>(); }, [] { __syncthreads(); });
+        } else {
+            get_q(0);
             wait_vm<0>();
-        }
-        __syncthreads();
-        for (int n = 0; n <= N; ++n) {
-            if constexpr (RING) {
-                __syncthreads();
-                if (DT < D && n + 1 < N) get_t(n + 1);
-                if (n + 2 < N) {
-                    get_q(n + 2); // (for step n + 1)
-                    get_k(n + 2);
-                    if (DT == D) get_t(n + 2);
-                }
-                __syncthreads();
-                // (the last ones asked for are those of step n + 2)
-                n + 2 < N ? wait_vm<LoadK::COUNT + (DT == D ? TB / 2048 : 0)>() : wait_vm<0>();
-            } else {
+            __syncthreads();
+            aim_touch(w2);
+            __syncthreads();
+            for (int n = 0; n <= N; ++n) {
                 if (n < N) {
                     get_k(n);
                     get_t(n);
