@@ -7,8 +7,10 @@
 // and with sums over the value heads of the key head
 //     dq = sum e^G dO' S^T + (sum W1) K        dk = sum (beta ec E D^T - e^G dV S^T) + (sum W2) K + (sum W1)^T Q + (sum W2)^T K
 // W1 and W2 are summed in 32 bits before their one rounding: what cancels between heads leaves no rounding behind, and the heads share
-// these products.  The pairs of dg_t are row sums and column sums of Z, taken from fp32 products: formed out of q.dq and k.dk instead, pairs
-// that cancel in exact arithmetic would leave the roundings of W behind.
+// these products.  The pairs of dg_t are sums of Z, taken from fp32 products: formed out of q.dq and k.dk instead, pairs that cancel in exact
+// arithmetic would leave the roundings of W behind.  They are those with i >= t > j and no others, tile by tile (row sums, column sums, and in a
+// tile on the diagonal sums over the rows from t on): all of them carry the decay of token t, so that dg_t is as exact behind a strong decay, and 0
+// where the decay is; as a running difference of all column sums and all row sums it would be off by the rounding of what the others leave.
 // One workgroup of four waves per (chunk, key head), which goes through its value heads; the states' parts of dq, dk and W1, W2 are summed in
 // workspace that only their own thread touches (in registers they would spill others).
 // A wave owns 32 of dk (with half of the tokens at dk = 64): its rows of S, D, K^T and Q^T are its A operands, straight
@@ -46,7 +48,7 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
     __shared__ __align__(16) T s_e[64 * 64], s_do[64 * 64], s_dv[64 * 64]; // halves of E, dO, dV
     __shared__ __align__(16) T s_w1[64 * 64], s_w2[64 * 64];               // W1, W2 kept [j][i]
     __shared__ __align__(16) float s_hi[64], s_lo[64], s_be[64], s_eg[64], s_ec[64];
-    __shared__ float s_row[4][64], s_col[2][4][64], s_a[4][64], s_b[4][64], s_tr[4];
+    __shared__ float s_row[4][64], s_col[4][64], s_a[4][64], s_b[4][64], s_tr[4];
 
     const int id = first + (int)blockIdx.x, hk = id % d.Hk, shared = SHARED ? d.H / d.Hk : 1;
     GdrChunk p = gdr_chunk(d, id / d.Hk, hk * shared);
@@ -175,15 +177,16 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
                 }
             }
         }
-        // (rows and columns of Z by tile: a tile's sums go to its own place, [other tile][token])
+        // (rows and columns of Z by tile: a tile's sums go to its own place, [other tile][token]; in a tile on the diagonal token i's place among the
+        // rows is for the tile's pairs i' >= i > j)
 #pragma unroll
         for (int u = 0; u < 3; ++u) {
             const int ta = pairs >> (4 * u + 2) & 3, tb = pairs >> (4 * u) & 3;
             if (u < 2 || w < 2) {
                 const int j = 16 * tb + r;
                 const float hj = s_hi[j], lj = s_lo[j], bj = s_be[j];
-                f32x4 w1, w2;
-                float below = 0.f, all = 0.f;
+                f32x4 w1, w2, zb;
+                float all = 0.f;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int i = 16 * ta + 4 * kg + x;
@@ -193,16 +196,27 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
                     w1[x] = bj * v1;
                     w2[x] = bj * v2;
                     all += z;
-                    below += i > j ? z : 0.f;
-                    const float zr = reduce16(i > j ? bj * z : 0.f);
-                    if (r == 0) s_row[tb][i] = zr;
+                    zb[x] = i > j ? bj * z : 0.f;
+                }
+                if (ta == tb) {
+#pragma unroll
+                    for (int x = 2; x >= 0; --x) zb[x] += zb[x + 1];
+                    float from = zb[0]; // over the rows of this lane group and those behind it
+                    const float x16 = __shfl_down(from, 16);
+                    from += kg < 3 ? x16 : 0.f;
+                    const float x32 = __shfl_down(from, 32);
+                    from += kg < 2 ? x32 : 0.f;
+                    const float next = __shfl_down(from, 16), behind = kg < 3 ? next : 0.f;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) zb[x] = r < 4 * kg + x ? zb[x] + behind : 0.f;
+                }
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float zr = reduce16(zb[x]);
+                    if (r == 0) s_row[tb][16 * ta + 4 * kg + x] = zr;
                 }
                 all = add_xor32(add_xor16(all));
-                below = add_xor32(add_xor16(below));
-                if (kg == 0) {
-                    s_col[0][ta][j] = all;
-                    s_col[1][ta][j] = below;
-                }
+                if (kg == 0) s_col[ta][j] = all;
                 if (SHARED && hs) {
                     w1 += sum[(NI * 4 + u) * 64];
                     w2 += sum[(NI * 4 + 3 + u) * 64];
@@ -251,24 +265,39 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
         __syncthreads();
         if (w == 0) { // dg, dbeta: lane = token
             const int tile = lane >> 4;
-            float row = 0.f, all = s_b[0][lane], below = 0.f, av = s_a[0][lane], bv = s_b[0][lane];
+            float all = s_b[0][lane], av = s_a[0][lane], bv = s_b[0][lane];
 #pragma unroll
             for (int n = 1; n < NP; ++n) {
                 av += s_a[n][lane];
                 bv += s_b[n][lane];
                 all += s_b[n][lane];
             }
+            // pairs of this tile's rows and the tiles in front of it, of this tile's columns and the tiles behind it, of neither
+            float rows_in = 0.f, cols_in = 0.f, to[4];
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                if (n <= tile) row += s_row[n][lane];
-                if (n >= tile) {
-                    all += s_col[0][n][lane];
-                    below += s_col[1][n][lane];
-                }
+                to[n] = n > tile ? be * s_col[n][lane] : 0.f;
+                cols_in += to[n];
+                if (n < tile) rows_in += s_row[n][lane];
+                if (n >= tile) all += s_col[n][lane];
             }
-            if (lane >= rows) row = below = av = bv = 0.f;
+            const float t2 = reduce16(to[2]), t3 = reduce16(to[3]);
+            const float across1 = lane_value(t2, 0) + lane_value(t3, 0), across2 = lane_value(t3, 0) + lane_value(t3, 16);
+            const float across = tile == 1 ? across1 : tile == 2 ? across2 : 0.f;
+            if (lane >= rows) av = bv = 0.f;
+            // sums inside the tile: over the rows from this token on, over the columns in front of it
+            rows_in += dpp_move<0x101>(rows_in); // row_shl 1, 2, 4, 8
+            rows_in += dpp_move<0x102>(rows_in);
+            rows_in += dpp_move<0x104>(rows_in);
+            rows_in += dpp_move<0x108>(rows_in);
+            cols_in = dpp_move<0x111>(cols_in); // row_shr 1; 1, 2, 4, 8
+            cols_in += dpp_move<0x111>(cols_in);
+            cols_in += dpp_move<0x112>(cols_in);
+            cols_in += dpp_move<0x114>(cols_in);
+            cols_in += dpp_move<0x118>(cols_in);
+            const float pairs_here = s_row[tile][lane] + rows_in + cols_in + across;
             // sums over the tokens before this one, and over this one and those behind it
-            float before = be * (below + bv) - row, behind = av;
+            float before = be * bv, behind = av;
 #pragma unroll
             for (int n = 1; n < 64; n *= 2) {
                 const float x = __shfl_up(before, n), y = __shfl_down(behind, n);
@@ -281,7 +310,7 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
 #pragma unroll
             for (int n = 1; n < NP; ++n) tr += s_tr[n];
             if (lane < rows) {
-                static_cast<T *>(a.dg)[gate] = from_f32<T>(before + behind + s_eg[63] * tr);
+                static_cast<T *>(a.dg)[gate] = from_f32<T>(pairs_here + before + behind + s_eg[63] * tr);
                 static_cast<T *>(a.dbeta)[gate] = from_f32<T>(all);
             }
         }
