@@ -223,9 +223,12 @@ int mdn_recurrent_step(const mdn_shape *shape, const void *q, const void *k, con
 typedef struct mdn_gdr_shape {
     int32_t B, T, H, Hk; /* batch, sequence length, value heads, key heads */
     int32_t dk, dv;
-    int32_t dtype;       /* MDN_DTYPE_* */
+    int32_t dtype;       /* MDN_DTYPE_*, or that + MDN_GDR_F32_GATE_GRADS */
     float scale;         /* multiplies q; usually dk^-1/2 */
 } mdn_gdr_shape;
+
+/* Added to mdn_gdr_shape.dtype: mdn_gdr_chunk_bwd writes dg and dbeta in fp32, as they are summed (the other calls do not go by it). */
+enum { MDN_GDR_F32_GATE_GRADS = 16 };
 
 enum { MDN_GDR_WS_FWD = 0, MDN_GDR_WS_BWD = 1, MDN_GDR_STATES = 2, MDN_GDR_OPERANDS = 3 };
 /* Bytes of the workspace of the forward / backward call and of the optional buffers states_saved and operands_saved.  Host-only. */
@@ -240,8 +243,9 @@ int mdn_gdr_chunk_fwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int
 /* Backward, for L = <o, dO> + <S_final, dS_final>, from the forward's inputs (v is not needed) and e_saved.  Without states_saved /
  * operands_saved (NULL) the backward forms them again; with dS0 asked for and 16-bit storage it forms the operands again in any case.
  * dS_final may be NULL (= 0), dS0 may be NULL (not wanted) or the memory of S0 or of dS_final.
- * dq, dk [B,T,Hk,dk] are summed over the value heads of a key head (in 32 bits), dv [B,T,H,dv]; dg, dbeta [B,T,H] are in the STORAGE dtype: what
- * products of 16-bit operands say about a gate is good to as many bits. */
+ * dq, dk [B,T,Hk,dk] are summed over the value heads of a key head (in 32 bits), dv [B,T,H,dv]; dg, dbeta [B,T,H] are in the STORAGE dtype, or with
+ * MDN_GDR_F32_GATE_GRADS fp32.  (With 16-bit operands one of them is good to about 8 bits either way; the rounding counts where many tokens'
+ * are summed into a parameter's gradient.) */
 int mdn_gdr_chunk_bwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int32_t n_seq, const void *q, const void *k, const float *g,
                       const float *beta, const float *S0, const void *e_saved, const void *states_saved, const void *operands_saved,
                       const void *dO, const float *dS_final, void *dq, void *dk, void *dv, void *dg, void *dbeta, float *dS0,

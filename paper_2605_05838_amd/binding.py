@@ -21,6 +21,7 @@ LIB_PATH = os.path.join(_HERE, "libmdn_hip.so")
 MDN_DTYPE_BF16, MDN_DTYPE_F32 = 0, 1
 MDN_WS_FWD, MDN_WS_BWD, MDN_WS_BWD_STATE_ADJOINTS = 0, 1, 2
 MDN_GDR_WS_FWD, MDN_GDR_WS_BWD, MDN_GDR_STATES, MDN_GDR_OPERANDS = 0, 1, 2, 3
+MDN_GDR_F32_GATE_GRADS = 16 # added to MdnGdrShape.dtype
 MDN_WS_FWD_NO_STATES, MDN_WS_BWD_NO_STATES, MDN_WS_BWD_NO_STATE_ADJOINTS = 3, 4, 5 # packed batches only
 
 EXPORTS = ("mdn_version", "mdn_strerror", "mdn_workspace_bytes", "mdn_saved_states_bytes",
@@ -319,12 +320,12 @@ def mdn_gdr_chunk_fwd(q, k, v, g, beta, S0=None, scale=None, cu_seqlens=None, sa
 
 
 def mdn_gdr_chunk_bwd(q, k, g, beta, e, dO, S0=None, states=None, operands=None, dS_final=None, scale=None, cu_seqlens=None,
-                      want_dS0=False, workspace=None, out=None):
+                      want_dS0=False, workspace=None, out=None, gate_dtype=None):
     """Adjoint of mdn_gdr_chunk_fwd from its inputs and its e (states, operands: the forward's, or formed again).  Returns a dict: dq, dk
-    (summed over the value heads of a key head), dv, dg, dbeta (all in q's dtype), dS0 (fp32 or None), workspace; `out`: such a dict, whose
-    tensors are reused."""
+    (summed over the value heads of a key head), dv, dg, dbeta (all in q's dtype; dg and dbeta with gate_dtype=torch.float32 in fp32, as they
+    are summed), dS0 (fp32 or None), workspace; `out`: such a dict, whose tensors are reused."""
     return (_host or _load_host()).gdr_chunk_bwd(q, k, g, beta, e, dO, S0, states, operands, dS_final, scale, cu_seqlens, want_dS0,
-                                                 workspace, out)
+                                                 workspace, out, gate_dtype)
 
 
 def mdn_gdr_recurrent_step(q, k, v, g, beta, S, scale=None, out=None):

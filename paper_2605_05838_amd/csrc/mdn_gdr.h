@@ -62,6 +62,7 @@ struct GdrGradArgs {
     const void *states, *dstates;
     void *sums; // H > Hk: gdr_sums_bytes() of workspace; otherwise null
     void *dq, *dk, *dg, *dbeta;
+    bool f32_gates; // dg, dbeta in fp32, not in the storage type
 };
 struct GdrStepArgs {
     const void *q, *k, *v;

@@ -26,7 +26,8 @@ struct Carve {
 
 int check_shape(const mdn_gdr_shape *s, GdrDims *d) {
     if (!s) return MDN_ERR_NULL;
-    if (s->dtype != MDN_DTYPE_BF16 && s->dtype != MDN_DTYPE_F32) return MDN_ERR_DTYPE;
+    const int dtype = s->dtype & ~MDN_GDR_F32_GATE_GRADS;
+    if (dtype != MDN_DTYPE_BF16 && dtype != MDN_DTYPE_F32) return MDN_ERR_DTYPE;
     if (s->B < 1 || s->T < 1 || s->H < 1 || s->Hk < 1 || s->H > 4096 || s->H % s->Hk) return MDN_ERR_SHAPE;
     if ((s->dk != 64 && s->dk != 128) || (s->dv != 64 && s->dv != 128)) return MDN_ERR_SHAPE;
     if ((long long)s->B * s->H > (1 << 24) || ((long long)s->B * s->T + 64) * s->H > (1LL << 31) - 1) return MDN_ERR_SHAPE;
@@ -35,7 +36,7 @@ int check_shape(const mdn_gdr_shape *s, GdrDims *d) {
     d->N = (int)(((long long)s->T + 63) / 64);
     d->cn = d->N;
     d->nchunks = (int)((long long)s->B * d->N);
-    d->dk = s->dk; d->dv = s->dv; d->dtype = s->dtype; d->scale = s->scale;
+    d->dk = s->dk; d->dv = s->dv; d->dtype = dtype; d->scale = s->scale;
     return MDN_OK;
 }
 
@@ -272,6 +273,7 @@ int mdn_gdr_chunk_bwd(const mdn_gdr_shape *shape, const int32_t *cu_seqlens, int
     GdrGradArgs c = {};
     c.q = q; c.k = k; c.e = e_saved; c.dO = dO; c.dv = dv; c.g = g; c.beta = beta; c.states = states_saved ? states_saved : w.states;
     c.dstates = w.dstates; c.sums = w.sums; c.dq = dq; c.dk = dk; c.dg = dg; c.dbeta = dbeta;
+    c.f32_gates = shape->dtype & MDN_GDR_F32_GATE_GRADS;
     const int nseg = segments(d, !states_saved, precise);
     if (nseg == 1) {
         if (!states_saved) { // before anything is written over S0

@@ -310,8 +310,14 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
 #pragma unroll
             for (int n = 1; n < NP; ++n) tr += s_tr[n];
             if (lane < rows) {
-                static_cast<T *>(a.dg)[gate] = from_f32<T>(pairs_here + before + behind + s_eg[63] * tr);
-                static_cast<T *>(a.dbeta)[gate] = from_f32<T>(all);
+                const float dg = pairs_here + before + behind + s_eg[63] * tr;
+                if (sizeof(T) == 4 || a.f32_gates) {
+                    static_cast<float *>(a.dg)[gate] = dg;
+                    static_cast<float *>(a.dbeta)[gate] = all;
+                } else {
+                    static_cast<T *>(a.dg)[gate] = from_f32<T>(dg);
+                    static_cast<T *>(a.dbeta)[gate] = from_f32<T>(all);
+                }
             }
         }
         if (SHARED) {

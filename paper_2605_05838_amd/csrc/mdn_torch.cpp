@@ -461,6 +461,14 @@ PyObject *chunk_bwd_varlen(PyObject *const *x) {
     return r.release();
 }
 
+// a torch.dtype argument
+at::ScalarType storage_type(PyObject *o, const char *name = "dtype") {
+    if (!THPDtype_Check(o)) fail(std::string(name) + " must be torch.bfloat16 or torch.float32");
+    const at::ScalarType t = reinterpret_cast<THPDtype *>(o)->scalar_type;
+    if (t != at::kBFloat16 && t != at::kFloat) fail(std::string(name) + " must be torch.bfloat16 or torch.float32");
+    return t;
+}
+
 // ---- the gated delta rule
 
 // the tensors' device as the current one while the call runs, and its stream
@@ -535,7 +543,7 @@ PyObject *gdr_chunk_fwd(PyObject *const *x) {
     return r.release();
 }
 
-// q k g beta e dO | S0 states operands dS_final scale cu_seqlens want_dS0 workspace out
+// q k g beta e dO | S0 states operands dS_final scale cu_seqlens want_dS0 workspace out gate_dtype
 PyObject *gdr_chunk_bwd(PyObject *const *x) {
     const GdrInputs in(x[0], x[1], x[4], "e", x[2], x[3], x[6], x[10], x[11]);
     const at::Tensor &dO = need(x[5], "dO");
@@ -545,15 +553,19 @@ PyObject *gdr_chunk_bwd(PyObject *const *x) {
     expect("dS_final", dS, {in.seqs, in.H, in.dk, in.dv}, at::kFloat, in.q);
     if (states) expect_bytes("states", states, in.bytes(MDN_GDR_STATES), in.q);
     if (operands) expect_bytes("operands", operands, in.bytes(MDN_GDR_OPERANDS), in.q);
+    const at::ScalarType gate_dt = x[15] && x[15] != Py_None ? storage_type(x[15], "gate_dtype") : in.dt;
+    if (gate_dt != in.dt && gate_dt != at::kFloat) fail("gate_dtype must be torch.float32 or q's dtype");
+    mdn_gdr_shape s = in.s;
+    if (gate_dt != in.dt) s.dtype |= MDN_GDR_F32_GATE_GRADS;
     PyObject *out = x[14];
     at::Tensor dq = output(out, "dq", {in.B, in.T, in.Hk, in.dk}, in.dt, in.q), dk = output(out, "dk", {in.B, in.T, in.Hk, in.dk}, in.dt, in.q),
-               dv = output(out, "dv", {in.B, in.T, in.H, in.dv}, in.dt, in.q), dg = output(out, "dg", {in.B, in.T, in.H}, in.dt, in.q),
-               db = output(out, "dbeta", {in.B, in.T, in.H}, in.dt, in.q);
+               dv = output(out, "dv", {in.B, in.T, in.H, in.dv}, in.dt, in.q), dg = output(out, "dg", {in.B, in.T, in.H}, gate_dt, in.q),
+               db = output(out, "dbeta", {in.B, in.T, in.H}, gate_dt, in.q);
     c10::optional<at::Tensor> dS0;
     if (truth(x[12])) dS0 = output(out, "dS0", {in.seqs, in.H, in.dk, in.dv}, at::kFloat, in.q);
     at::Tensor ws = workspace(x[13], need_ws, in.q);
     const OnDevice dev(in.q);
-    call("mdn_gdr_chunk_bwd", mdn_gdr_chunk_bwd, &in.s, in.offs(), in.n_offs(), ptr(in.q), ptr(in.k), ptr<float>(in.g), ptr<float>(in.beta),
+    call("mdn_gdr_chunk_bwd", mdn_gdr_chunk_bwd, static_cast<const mdn_gdr_shape *>(&s), in.offs(), in.n_offs(), ptr(in.q), ptr(in.k), ptr<float>(in.g), ptr<float>(in.beta),
          ptr<float>(in.S0), ptr(in.v), ptr(states), ptr(operands), ptr(dO), ptr<float>(dS), ptr(dq), ptr(dk), ptr(dv), ptr(dg), ptr(db),
          ptr<float>(dS0), ptr(ws), size_of(ws), dev.stream);
     Dict r;
@@ -805,13 +817,6 @@ mdn_shape rows_shape(const at::Tensor &x, int dtype) {
         if (n > 0x7fffffff) fail("sizes must fit 32 bits");
     return mdn_shape{(int32_t)x.size(0), (int32_t)x.size(1), (int32_t)x.size(2), (int32_t)x.size(3), (int32_t)x.size(3), 64, dtype, 1.f};
 }
-// a torch.dtype argument
-at::ScalarType storage_type(PyObject *o) {
-    if (!THPDtype_Check(o)) fail("dtype must be torch.bfloat16 or torch.float32");
-    const at::ScalarType t = reinterpret_cast<THPDtype *>(o)->scalar_type;
-    if (t != at::kBFloat16 && t != at::kFloat) fail("dtype must be torch.bfloat16 or torch.float32");
-    return t;
-}
 int code_of(at::ScalarType t) { return t == at::kFloat ? MDN_DTYPE_F32 : MDN_DTYPE_BF16; }
 size_t kept_workspace(const mdn_shape &s) {
     size_t n = 0;
@@ -1011,7 +1016,7 @@ PyMethodDef methods[] = {MDN_ENTRY(chunk_fwd, 17), MDN_ENTRY(chunk_fwd_noalloc, 
                          MDN_ENTRY(recurrent_step, 11), MDN_ENTRY(chunk_fwd_varlen, 13), MDN_ENTRY(chunk_bwd_varlen, 17),
                          MDN_ENTRY(gates_fwd, 11), MDN_ENTRY(gates_bwd, 16), MDN_ENTRY(frontend_fwd, 5),
                          MDN_ENTRY(frontend_bwd, 9), MDN_ENTRY(epilogue_fwd, 4), MDN_ENTRY(epilogue_bwd, 6),
-                         MDN_ENTRY(gdr_chunk_fwd, 14), MDN_ENTRY(gdr_chunk_bwd, 15), MDN_ENTRY(gdr_recurrent_step, 8),
+                         MDN_ENTRY(gdr_chunk_fwd, 14), MDN_ENTRY(gdr_chunk_bwd, 16), MDN_ENTRY(gdr_recurrent_step, 8),
                          MDN_ENTRY(keep, 1), MDN_ENTRY(kept_values, 2), MDN_ENTRY(frontend_fwd_keep, 5), MDN_ENTRY(frontend_fwd_kept, 6),
                          MDN_ENTRY(frontend_bwd_kept, 9), MDN_ENTRY(epilogue_fwd_keep, 4), MDN_ENTRY(epilogue_bwd_kept, 6),
                          {"set_error_types", set_error_types, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
