@@ -9,6 +9,7 @@
 // waves and workgroups one after the other; dd as a value per row, then over slabs of tokens.
 // Bound by HBM, 4 x 4 096 tokens of 16 heads of 128 in 16 bits: front end with checkpoints 98 us (5.1 TB/s), from them 69 (4.4), its backward 106
 // (4.8); back end with checkpoints 56 (4.8), its backward 64 (4.2).
+#include "mdn_kept_rules.h"
 #include "mdn_layer_rows.h"
 
 namespace mdn {
@@ -309,11 +310,8 @@ template <int N> bool kept_set(const mdn_kept *k, KeptSet<N> *s) {
     return true;
 }
 
-// slabs of the sums over tokens: one (and one launch) while that takes less than a second launch would
-constexpr int kSlabs = 128;
-int slabs(const LayerDims &d) { return d.rows <= 16384u ? 1 : kSlabs; }
 constexpr int kMaxCus = 1024; // of a device
-size_t front_ws(const LayerDims &d) { return ((size_t)d.rows + (size_t)kSlabs * d.H) * sizeof(float); }
+size_t front_ws(const LayerDims &d) { return ((size_t)d.rows + (size_t)kMaxSlabs * d.H) * sizeof(float); }
 size_t back_ws(int D) { return (size_t)kMaxCus * D * sizeof(float); }
 bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 3u; }
 
@@ -423,7 +421,7 @@ int mdn_frontend_bwd_kept(const mdn_shape *shape, const mdn_kept *kept, const fl
         return status();
     });
     if (rc || !dd) return rc;
-    const int tokens = (int)(ld.rows / (unsigned)ld.H), n = slabs(ld);
+    const int tokens = (int)(ld.rows / (unsigned)ld.H), n = kept_slabs(ld.rows, ld.H);
     float *parts = n == 1 ? dd : rows + ld.rows;
     hipLaunchKernelGGL(sum_tokens_kernel, dim3(n), dim3(kSumThreads), 0, s, rows, parts, tokens, ld.H);
     if (n > 1) hipLaunchKernelGGL(sum_tokens_kernel, dim3(1), dim3(kSumThreads), 0, s, parts, dd, n, ld.H);
