@@ -76,6 +76,15 @@ __device__ __forceinline__ float lane_value(float v, int src) {
 }
 __device__ __forceinline__ int wave_id() { return threadIdx.x >> 6; }
 
+// A barrier that this wave reaches with all of its LDS operations done.  (A loop whose first statement is __syncthreads() has been compiled to one
+// that does not wait: the wait is dropped when the loop is entered without anything outstanding, and the LDS writes that come around from
+// the loop's end meet the barrier unfinished.  The reverse scan then stored rows of the step before.  tests/test_compiled_barriers.py looks at
+// every barrier as it is compiled.)
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    __syncthreads();
+}
+
 // acc[nt] += A(16 x K) * B(K x 16*NT)
 //   A(m, k)  = A[m * lda + k]          (16 rows starting at A)
 //   B(k, n)  = Bt[n * ldb + k]         (16*NT columns starting at Bt)

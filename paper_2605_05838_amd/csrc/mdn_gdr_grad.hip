@@ -77,7 +77,7 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
         const int h = hk * shared + hs;
         if (hs) {
             p = gdr_chunk(d, id / d.Hk, h);
-            __syncthreads(); // everything in LDS of the head before is done with
+            lds_barrier(); // everything in LDS of the head before is done with
         }
         const size_t gate = (p.tok + min(lane, rows - 1)) * d.H + h, val = (p.tok * d.H + h) * DV;
         float g = a.g[gate], be = a.beta[gate];
@@ -120,12 +120,12 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
             // In 16 bits asked for before the tiles, so that one wait covers both: 183 us for 200, [4, 4 096] tokens, 16 heads, d = 128
             Frag sf[S64][2], df[S64][2];
             states(sf, df, hv);
-            if (hv) __syncthreads(); // the tiles before these are done with
+            if (hv) lds_barrier(); // the tiles before these are done with
             tile(TileV{}, s_e, static_cast<const T *>(a.e) + val + hv * 64, rsv);
             tile(TileV{}, s_do, static_cast<const T *>(a.dO) + val + hv * 64, rsv);
             tile(TileV{}, s_dv, static_cast<const T *>(a.dv) + val + hv * 64, rsv);
             wait_vm<0>();
-            __syncthreads();
+            lds_barrier();
             // dO E^T, dV E^T
 #pragma unroll
             for (int u = 0; u < 3; ++u) {
@@ -262,7 +262,7 @@ template <typename T, int DK, int DV, bool SHARED> __global__ __launch_bounds__(
                 s_b[part][tok] = bv;
             }
         }
-        __syncthreads();
+        lds_barrier();
         if (w == 0) { // dg, dbeta: lane = token
             const int tile = lane >> 4;
             float all = s_b[0][lane], av = s_a[0][lane], bv = s_b[0][lane];

@@ -79,7 +79,7 @@ template <typename T, int DK> __global__ __launch_bounds__(kThreads, sizeof(T) =
         c[64 + lane] = be * GdrDecay::pow2(hC - dec.hi, lC - dec.lo);
     }
     wait_vm<0>();
-    __syncthreads();
+    lds_barrier();
 
     auto row_frag = [&](const T *t, int row, int st) {
         return O::load(t + row * DK + ((st * 4 + kg) ^ (row & XM)) * Gd<T>::E);
@@ -100,7 +100,7 @@ template <typename T, int DK> __global__ __launch_bounds__(kThreads, sizeof(T) =
             }
         }
     }
-    __syncthreads();
+    lds_barrier();
     auto put = [&](int ta, int tb, f32x4 kv, f32x4 qv) {
         const int j = 16 * tb + r;
         const float hj = s_hi[j], lj = s_lo[j], bj = s_be[j];
@@ -122,9 +122,9 @@ template <typename T, int DK> __global__ __launch_bounds__(kThreads, sizeof(T) =
             sA[i * LDM + j] = sP[i * LDM + j] = 0.f;
         }
     }
-    __syncthreads();
+    lds_barrier();
     tri_inverse_blocked(sA, LDM, w);
-    __syncthreads();
+    lds_barrier();
     put_triangle<T, false>(sA, a.T, a.T_lo, p.blk);
     put_triangle<T, false>(sP, a.P, nullptr, p.blk);
     put_triangle<T, true>(sA, a.TT, a.TT_lo, p.blk);

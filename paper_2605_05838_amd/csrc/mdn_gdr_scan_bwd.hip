@@ -75,12 +75,12 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
     if (w >= STORES) {
         const int w2 = w - STORES;
         aim_touch(w2);
-        __syncthreads();
-        __syncthreads();
+        lds_barrier();
+        lds_barrier();
         for (int n = 0; n <= N; ++n) {
-            __syncthreads();
+            lds_barrier();
             if (n) store(n - 1, w2);
-            __syncthreads();
+            lds_barrier();
             touch.chunk(N - 1 - n - kTouchAhead, s_touch[w2]);
         }
         wait_vm<0>();
@@ -110,13 +110,13 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
         if constexpr (RING) {
             // (requests of K and T^T by either wave)
             constexpr int LAST = LoadK::COUNT + (DT == D ? TB / 2048 : 0);
-            reverse_ring<DT>(N, get_q, get_k, get_t, [](bool all) { all ? wait_vm<0>() : wait_vm<LAST>(); }, [] { __syncthreads(); });
+            reverse_ring<DT>(N, get_q, get_k, get_t, [](bool all) { all ? wait_vm<0>() : wait_vm<LAST>(); }, [] { lds_barrier(); });
         } else {
             get_q(0);
             wait_vm<0>();
-            __syncthreads();
+            lds_barrier();
             aim_touch(w2);
-            __syncthreads();
+            lds_barrier();
             for (int n = 0; n <= N; ++n) {
                 if (n < N) {
                     get_k(n);
@@ -124,11 +124,11 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
                 }
                 if (n + 1 < N) get_q(n + 1);
                 wait_vm<0>();
-                __syncthreads();
+                lds_barrier();
                 if (n) store(n - 1, w2); // (and stores, while the others multiply)
-                __syncthreads();
+                lds_barrier();
                 touch.chunk(N - 1 - n - kTouchAhead, s_touch[w2]);
-                __syncthreads();
+                lds_barrier();
             }
             wait_vm<0>();
         }
@@ -157,10 +157,10 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
             publish(0);
         }
         if (lane == 0) s_said[cg][TW] = 0;
-        __syncthreads();
-        __syncthreads();
+        lds_barrier();
+        lds_barrier();
         for (int n = 0; n <= N; ++n) {
-            __syncthreads();
+            lds_barrier();
             if (n < N) {
                 const T *k = s_k[slot], *tri = s_t[slot_t], *tri_lo = s_tl[slot_t];
                 const float *c = s_c[slot_c] + G::row(0, 4 * kg);
@@ -178,7 +178,7 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
                 const float eC = s_c[slot_c][63];
 #pragma unroll
                 for (int t = 0; t < HT; ++t) S[t] = eC * S[t] + s_y[cg][TW * HT + t][lane];
-                __syncthreads();
+                lds_barrier();
                 if constexpr (CWS == 1) publish(n);
                 f32x4 E[RT];
                 zero_acc(E);
@@ -264,9 +264,9 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
                 slot_t = next_slot<DT>(slot_t);
                 slot_c = next_slot<DC>(slot_c);
             } else {
-                __syncthreads();
+                lds_barrier();
             }
-            if constexpr (!RING) __syncthreads();
+            if constexpr (!RING) lds_barrier();
         }
         if (a.dS0) save_state<T, TW * HT>(S, a.dS0 + q.state * DK * d.dv, d.dv, col, r, kg);
     };
@@ -353,20 +353,20 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
 #pragma unroll
         for (int i = 0; i < SETS; ++i) fetch(sets[i], i);
         all_arrived();
-        __syncthreads();
+        lds_barrier();
         ahead(sets[0], 0);
-        __syncthreads();
+        lds_barrier();
         auto turn = [&](Set &x, int n) {
-            __syncthreads();
-            __syncthreads();
+            lds_barrier();
+            lds_barrier();
             ahead(x, n + 1);
-            if constexpr (!RING) __syncthreads();
+            if constexpr (!RING) lds_barrier();
         };
         // step 0
-        __syncthreads();
-        __syncthreads();
+        lds_barrier();
+        lds_barrier();
         if (N > 1) ahead(sets[SETS - 1], 1);
-        if constexpr (!RING) __syncthreads();
+        if constexpr (!RING) lds_barrier();
         // steps 1 .. N - 2, whole turns without a branch inside (the compiler counts the loads in flight): X, Y of steps 2 .. N - 1
         int n = 1;
         for (; n + SETS <= N - 1; n += SETS)
@@ -375,9 +375,9 @@ __global__ __launch_bounds__((bwd_waves<T, DK, NCG, PRECISE>() * 64)) void gdr_s
         if (n <= N - 2) turn(sets[0], n++);
         // the last two steps: nothing is ahead of them
         for (; n <= N; ++n) {
-            __syncthreads();
-            __syncthreads();
-            if constexpr (!RING) __syncthreads();
+            lds_barrier();
+            lds_barrier();
+            if constexpr (!RING) lds_barrier();
         }
     };
     if (w == 0) beside(std::integral_constant<int, 0>{});

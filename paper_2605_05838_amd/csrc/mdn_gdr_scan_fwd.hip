@@ -103,7 +103,7 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
         const int w2 = w - STORES;
         aim_touch(w2);
         for (int n = 0; n <= N + 1; ++n) {
-            __syncthreads();
+            lds_barrier();
             store(n, w2);
             touch.chunk(n + kTouchAhead, s_touch[w2]);
         }
@@ -131,10 +131,10 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
             for (int n = 0; n <= N + 1; ++n) { // (and stores, while the others multiply)
                 if (n < N) request(n);
                 wait_vm<0>();
-                __syncthreads();
+                lds_barrier();
                 store(n, w2);
                 touch.chunk(n + kTouchAhead, s_touch[w2]);
-                __syncthreads();
+                lds_barrier();
             }
             wait_vm<0>();
         } else {
@@ -149,7 +149,7 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
                 wait_vm<0>();
             }
             for (int n = 0; n <= N + 1; ++n) {
-                __syncthreads();
+                lds_barrier();
                 if (n + 2 < N) {
                     request(n + 2);
                     all_but_last();
@@ -185,7 +185,7 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
         if constexpr (CWS == 2) publish();
         if (lane == 0) s_said[cg][TW] = 0;
         for (int n = 0; n <= N + 1; ++n) {
-            __syncthreads();
+            lds_barrier();
             if (n < N) {
                 const T *k = s_k[slot], *v = s_v[slot], *tri = s_t[slot], *tri_lo = s_tl[slot];
                 const float *c = s_c[slot_c] + G::row(0, 4 * kg);
@@ -281,7 +281,7 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
                 if (BEHIND) Sb.from(S);
                 if constexpr (CWS == 2) publish();
             }
-            if constexpr (D == 1) __syncthreads();
+            if constexpr (D == 1) lds_barrier();
         }
         if (a.S_final) save_state<T, TW * HT>(S, a.S_final + q.state * DK * d.dv, d.dv, col, r, kg);
     };
@@ -362,20 +362,20 @@ __global__ __launch_bounds__((fwd_waves<T, DK, NCG, PRECISE, REBUILD>() * 64)) v
 #pragma unroll
         for (int i = 0; i < SETS; ++i) fetch(sets[i], i);
         all_arrived();
-        __syncthreads();
-        if constexpr (D == 1) __syncthreads();
+        lds_barrier();
+        if constexpr (D == 1) lds_barrier();
         auto turn = [&](Set &x, int m) {
-            __syncthreads();
+            lds_barrier();
             step(x, m);
-            if constexpr (D == 1) __syncthreads();
+            if constexpr (D == 1) lds_barrier();
         };
         int m = 0;
         for (; m + SETS <= N; m += SETS) // (whole turns, without a branch inside: the compiler counts the loads in flight)
 #pragma unroll
             for (int i = 0; i < SETS; ++i) turn(sets[i], m + i);
         if (m < N) turn(sets[0], m);
-        __syncthreads();
-        if constexpr (D == 1) __syncthreads();
+        lds_barrier();
+        if constexpr (D == 1) lds_barrier();
     };
     if constexpr (!REBUILD) {
         if (w == 0) beside(std::integral_constant<int, 0>{});

@@ -59,7 +59,7 @@ template <typename T, int DK, int COLS, bool NT> __global__ __launch_bounds__(kT
         }
         part = sum(part);
         if ((threadIdx.x & 63) < CG) s_e[w][cg] = part;
-        __syncthreads();
+        lds_barrier();
         f32x4 e = widen4(c.v) - ((s_e[0][cg] + s_e[1][cg]) + (s_e[2][cg] + s_e[3][cg]));
         e *= c.be;
         f32x4 po = {0.f, 0.f, 0.f, 0.f};
@@ -70,7 +70,7 @@ template <typename T, int DK, int COLS, bool NT> __global__ __launch_bounds__(kT
         }
         po = sum(po);
         if ((threadIdx.x & 63) < CG) s_o[w][cg] = po;
-        __syncthreads();
+        lds_barrier();
         if (sl == 0) {
             const f32x4 o = (s_o[0][cg] + s_o[1][cg]) + (s_o[2][cg] + s_o[3][cg]);
             store4(static_cast<T *>(a.o) + (((size_t)b * d.T + t) * d.H + h) * d.dv + j, d.scale * o);
