@@ -234,10 +234,9 @@ inline bool gdr_touch_pays(const GdrDims &d, int key_rows, int value_rows, bool 
     return (size_t)d.nchunks * d.H * block > 5 * kLastLevelCache / 4;
 }
 
-// 16 columns per workgroup while there is a CU for each of these workgroups, or 32.  Calls in us, 16 / 32 columns, heads of 128: forward with
-// kept states, with final states, backward, with adjoints of the initial states: 777 tokens of 16 heads 24.5 / 25.3, 28.9 / 33.3, 33.2 / 35.8, 49 / 54;
-// 2 x 2 048 (256 workgroups of 16 columns) 55.2 / 55.7, 67 / 75, 83 / 88, 120 / 128; 3 x 2 048 (384) 93 / 65, 114 / 83, 141 / 107, 206 / 157;
-// 8 x 2 048 262 / 200, 239 / 165, 338 / 277, 479 / 384; heads of 64, where two would share a CU, 8 x 2 048 (512) 109 / 87, 113 / 85, 149 / 135, 223 / 184.
-inline bool gdr_one_group(const GdrDims &d) { return (long long)(d.B * d.H + 7) / 8 * 8 * (d.dv / 16) <= num_cus(); }
+// which of its two forms a scan takes: see sixteen_columns
+inline bool gdr_one_group(const GdrDims &d) {
+    return sixteen_columns(d.B, d.seqs ? d.nchunks : 0, d.N, d.H, d.dv, num_cus());
+}
 
 } // namespace mdn

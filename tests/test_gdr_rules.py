@@ -1,0 +1,40 @@
+"""The rule by which a scan of the gated delta rule takes 16 or 32 columns a workgroup (csrc/mdn_scan_rules.h), compiled for the host."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2605_05838_amd", "csrc")
+
+
+@pytest.fixture(scope="module")
+def sixteen(tmp_path_factory):
+    tmp = tmp_path_factory.mktemp("rules")
+    (tmp / "rules.cpp").write_text("""
+#include "mdn_scan_rules.h"
+extern "C" bool sixteen(size_t sequences, size_t chunks, size_t longest, size_t heads, int dv) {
+    return mdn::sixteen_columns(sequences, chunks, longest, heads, dv, 256);
+}
+""")
+    so = str(tmp / "rules.so")
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I" + CSRC, "-o", so, str(tmp / "rules.cpp")], check=True)
+    lib = ctypes.CDLL(so)
+    lib.sixteen.restype = ctypes.c_bool
+    lib.sixteen.argtypes = 4 * [ctypes.c_size_t] + [ctypes.c_int]
+    return lib.sixteen
+
+
+@pytest.mark.parametrize("B,T,H,dv,columns", [(1, 777, 16, 128, 16), (2, 2048, 16, 128, 16), (3, 2048, 16, 128, 32), (8, 2048, 16, 128, 32),
+                                              (8, 2048, 16, 64, 32), (1, 1, 4096, 64, 32), (1, 32768, 33, 128, 32), (1, 1, 32, 128, 16)])
+def test_equal_lengths(sixteen, B, T, H, dv, columns):
+    assert sixteen(B, 0, (T + 63) // 64, H, dv) is (columns == 16)
+
+
+@pytest.mark.parametrize("lens,columns", [([16384] + [64] * 20, 16), ([4096] + [64] * 20, 16), ([4096] + [512] * 20, 32),
+                                          ([4096, 2048, 1024] + [300] * 10, 32), ([8192] * 2 + [32] * 40, 32), ([777] * 3, 32), ([777], 16),
+                                          ([1] * 300, 32)])
+def test_packed_where_it_was_faster(sixteen, lens, columns):
+    """16 heads of 128: sequences beside one long one count by what there is to do beside it."""
+    chunks = [(n + 63) // 64 for n in lens]
+    assert sixteen(len(lens), sum(chunks), max(chunks), 16, 128) is (columns == 16)

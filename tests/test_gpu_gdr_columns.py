@@ -58,3 +58,16 @@ def test_packed(dtype, dk, dv):
             got = run(x, cu=cu, states=states, keep=keep)
             for key, w in want.items():
                 check(part(got, None, key, cu), w, dtype, (states, keep, key))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(64, 128), (128, 64)])
+def test_one_long_sequence_among_short_ones(dtype, dk, dv):
+    """More sequences than 16 columns are taken for where they are of equal lengths; by the longest one they are."""
+    lens = [20] * 9 + [1500] + [1, 64, 70] * 4
+    cu = np.cumsum([0] + lens).tolist()
+    x = inputs(dtype, T=cu[-1], H=4, Hk=2, dk=dk, dv=dv, seqs=len(lens), seed=5)
+    for states in (False, True):
+        want = oracle(part(x, None, 1, cu), cu=cu, states=states)
+        for keep in ((True, True), (False, False)):
+            check(part(run(x, cu=cu, states=states, keep=keep), None, 1, cu), want, dtype, (states, keep))
