@@ -11,6 +11,12 @@
 // group kg (`Gd::row`), a lane's accumulators of two tiles, rounded, ARE the B fragment of the product that contracts over those rows.
 // So states, corrections and their adjoints go from product to product without leaving the registers: no LDS round trip and
 // no barrier is on the chain of a chunk, whose products take their A operands from token tiles in LDS.
+//
+// What is rounded to the storage type: what the tensors hold, the kept states and adjoints, and the products' operands (S, T, P, V - e^G K S, E, D, dE,
+// dV, W); sums, decays, the inverse and the states along a chain are fp32.  With 16 bits against fp64, rms: o, e, dq, dk 2.9e-3, dv 1.7e-3, dg 2.4e-3 to
+// 4.2e-3, dbeta 2.3e-3 to 3.6e-3 (64 to 1 000 tokens, adjoints of the final states of any size), where rounding an exact result once leaves 1.7e-3; fp32
+// products run at an eighth of the rate or less, and operands of value + remainder, which states that leave the call in 32 bits are carried with (3e-6),
+// take two or three products for one.
 #pragma once
 #include "mdn_device.h"
 #include "mdn_kernels.h"

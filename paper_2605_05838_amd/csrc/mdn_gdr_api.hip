@@ -151,13 +151,13 @@ BwdWs carve_bwd(const GdrDims &d, bool packed, void *ws) {
 // A boundary costs ~10 us and hides a gradient launch, 40 us per 1 024 chunk blocks of d = 128: a segment per 1 024, at most 4; where the states are
 // reconstructed, which the gradient launches wait for, 2, but with remainders, whose scans take longer, as many.  Backward in us, 1 / 2 / 4 / 8
 // segments, states kept; reconstructed; reconstructed, with dS0 (16 heads of 128 unless said):
-//    4 096 tokens    117 /   128 /   142 /   182;     170 /   149 /   173 /   230;     211 /   212 /   220 /   233
-//    8 192           231 /   228 /   228 /   261;     330 /   260 /   277 /   321;     418 /   388 /   371 /   404
-//   16 384           465 /   425 /   404 /   430;     677 /   499 /   522 /   558;     867 /   741 /   706 /   721
-//   32 768           915 /   810 /   761 /   761;   1 349 /   948 /   984 / 1 032;   1 767 / 1 441 / 1 341 / 1 337
-//   32 768, 4 heads  672 /   665 /   668 /   704;     960 /   693 /   685 /   731;   1 287 / 1 060 / 1 050 / 1 082
-//   65 536, d = 64 1 332 / 1 260 / 1 227 / 1 247;   2 019 / 1 585 / 1 560 / 1 608;   2 594 / 2 035 / 1 946 / 1 962
-//    4 096, 8, fp32  361 /   348 /   372 /   441;     497 /   374 /   394 /   556;     498 /   421 /   397 /   556
+//    4 096 tokens    119 /   130 /   145 /   184;     172 /   151 /   174 /   232;     212 /   212 /   220 /   234
+//    8 192           236 /   232 /   233 /   264;     334 /   262 /   280 /   325;     418 /   390 /   372 /   406
+//   16 384           472 /   428 /   410 /   438;     685 /   499 /   526 /   558;     868 /   743 /   706 /   716
+//   32 768           931 /   822 /   766 /   767;   1 366 /   957 /   985 / 1 039;   1 770 / 1 446 / 1 346 / 1 333
+//   32 768, 4 heads  686 /   679 /   680 /   716;     976 /   704 /   700 /   745;   1 289 / 1 060 / 1 049 / 1 087
+//   65 536, d = 64 1 336 / 1 269 / 1 237 / 1 255;   2 021 / 1 598 / 1 555 / 1 618;   2 601 / 2 043 / 1 952 / 1 972
+//    4 096, 8, fp32  363 /   351 /   374 /   444;     500 /   375 /   394 /   557;     501 /   426 /   400 /   557
 int segments(const GdrDims &d, bool rebuild, bool precise) {
     if (d.seqs) return 1;
     long long k = requested_segments();

@@ -3,8 +3,10 @@
 // One workgroup of four waves per (chunk, value head).  The ten 16x16 tiles on and below the diagonal of K K^T and Q K^T are dealt
 // to the waves in pairs that share a B fragment; the inverse is fp32 whatever the storage.  T, P and their transposes leave as the
 // fragments that the scans load (mdn_gdr.h), triangles only: 6 KB each of 16-bit storage.  The K and Q tiles, dead after the
-// products, make room for A and P: 37 KB of LDS, four workgroups per CU.  Bound by HBM: 4 x 4 096 tokens of 16 heads of 128, all four
-// triangles written, 54 us for 230 MB, 4.3 TB/s.
+// products, make room for A and P: 37 KB of LDS, four workgroups per CU.  Bound by HBM where all four
+// triangles are written and every value head has a key head of its own: 4 x 4 096 tokens of 16 heads of 128, 53 us for 240 MB, 4.5 TB/s.  Where
+// only T and P are and heads share their keys, by what a chunk's phases wait for of each other: 16 384 tokens of 16 heads on 4 42.5 us for 86 MB, LDS
+// in use 45 % of a CU's clocks, MFMA 16 %; on 16, twice the bytes, 44.0.
 #include "mdn_coef.h"
 #include "mdn_gdr.h"
 

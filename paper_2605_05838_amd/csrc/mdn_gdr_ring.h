@@ -13,9 +13,9 @@ constexpr int reverse_t(bool precise) { return precise ? 2 : 3; }
 // ring of two) and q, dO of step n + 2.
 // q(n), k(n), t(n) ask for step n's; wait(false) waits for everything but the last k and, in a ring of three, t asked for; wait(true) for
 // everything.  Requests arrive in order: at the end of step n all that the next one works on is there, and K and T^T of step n + 2 have
-// that one's time as well.  (What a step needs is there early where later chunks' lines are in the L2, or the chain is what a step waits for: waiting
-// for everything at the end of every step takes as long, 911 us for 912 the backward call of 32 768 tokens of 16 heads of 128, 230.8 / 230.9 of
-// 8 192, 1 365 / 1 366 with remainders, 67.6 / 67.7 in fp32 ([2, 1 024] tokens, 4 heads, d = 64).)
+// that one's time as well.  (Most of what a step needs is there early, out of the L2: waiting for everything at the end of every step takes 932 us for 926,
+// the backward call of 32 768 tokens of 16 heads of 128, 236 for 235 of 8 192, 1 371 for 1 369 with remainders, 67.5 for 67.8 in fp32 ([2, 1 024]
+// tokens, 4 heads, d = 64).)
 template <int T, class Q, class K, class Tt, class Wait, class Barrier>
 __attribute__((always_inline)) constexpr void reverse_ring(int N, Q &&q, K &&k, Tt &&t, Wait &&wait, Barrier &&barrier) {
     q(0);

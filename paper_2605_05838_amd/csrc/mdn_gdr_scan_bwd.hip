@@ -13,7 +13,7 @@ namespace mdn {
 namespace {
 
 // Waves to 16 columns of the chain, as in the forward scan, two for one, backward calls: 68 us for 84 in fp32 (2 x 1 024 tokens, 4 heads, d = 64),
-// 916 for 1 221 (8 192 of 16, d = 128), with remainders 49 for 52 (777 tokens, 16 heads, d = 128), 1 366 for 1 449 (32 768).  (Not with 32
+// 919 for 1 223 (8 192 of 16, d = 128), with remainders 49 for 52 (777 tokens, 16 heads, d = 128), 1 369 for 1 455 (32 768).  (Not with 32
 // columns, whose LDS is full.)
 template <typename T, int NCG, bool PRECISE> constexpr int CW = (sizeof(T) == 4 || PRECISE) && NCG == 1 ? 2 : 1;
 // beside the chain, chain, loads, stores

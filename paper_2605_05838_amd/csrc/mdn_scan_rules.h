@@ -46,13 +46,13 @@ constexpr bool q_tile_pays(int columns, int d, size_t pairs, size_t chunks, size
 
 // Gated delta rule: 16 columns per workgroup while there is a CU for each of these workgroups, or 32.  `sequences` of `chunks` chunks together
 // (0: of equal lengths), the longest of `longest`.  Calls in us, 16 / 32 columns, heads of 128: forward with kept states, with final states,
-// backward, with adjoints of the initial states: 777 tokens of 16 heads 24.5 / 25.3, 28.9 / 33.3, 33.2 / 35.8, 49 / 54;
-// 2 x 2 048 (256 workgroups of 16 columns) 55.2 / 55.7, 67 / 75, 83 / 88, 120 / 128; 3 x 2 048 (384) 93 / 65, 114 / 83, 141 / 107, 206 / 157;
-// 8 x 2 048 262 / 200, 239 / 165, 338 / 277, 479 / 384; heads of 64, where two would share a CU, 8 x 2 048 (512) 109 / 87, 113 / 85, 149 / 135, 223 / 184.
+// backward, with adjoints of the initial states: 777 tokens of 16 heads 22.8 / 23.8, 28.0 / 32.7, 33.6 / 35.9, 49 / 54;
+// 2 x 2 048 (256 workgroups of 16 columns) 50 / 52, 62 / 73, 84 / 89, 119 / 128; 3 x 2 048 (384) 90 / 60, 115 / 81, 143 / 108, 205 / 157;
+// 8 x 2 048 246 / 147, 238 / 160, 341 / 278, 479 / 385; heads of 64, where two would share a CU, 8 x 2 048 (512) 100 / 77, 109 / 79, 149 / 135, 223 / 184.
 // Packed sequences count by the longest one: what is to be done beside its chain is the others' chunks, not their number.  16 heads of 128,
-// 16 384 and 20 x 64 tokens 380 / 382, 428 / 487, 531 / 577, 709 / 786; 4 096 and 20 x 64 91 / 91, 116 / 135, 157 / 169, 199 / 217; 4 096 and
-// 20 x 512 215 / 129, 236 / 159, 359 / 307, 445 / 355; 4 096, 2 048, 1 024 and 10 x 300 129 / 106, 165 / 147, 258 / 241, 316 / 290; 2 x 8 192 and
-// 40 x 32 322 / 255, 343 / 288, 479 / 428, 604 / 555; 3 x 777 43 / 30, 55 / 39, 82 / 68, 100 / 79.
+// 16 384 and 20 x 64 tokens 382 / 382, 434 / 485, 541 / 579, 711 / 787; 4 096 and 20 x 64 91 / 91, 116 / 135, 159 / 169, 199 / 217; 4 096 and
+// 20 x 512 216 / 127, 236 / 162, 362 / 308, 445 / 356; 4 096, 2 048, 1 024 and 10 x 300 128 / 105, 166 / 147, 260 / 242, 317 / 291; 2 x 8 192 and
+// 40 x 32 323 / 255, 344 / 289, 484 / 429, 605 / 557; 3 x 777 43 / 30, 56 / 40, 84 / 69, 100 / 80.
 constexpr bool sixteen_columns(size_t sequences, size_t chunks, size_t longest, size_t heads, int dv, size_t cus) {
     const size_t beside = chunks ? (chunks + longest - 1) / longest : sequences;
     return (beside * heads + 7) / 8 * 8 * (size_t)(dv / 16) <= cus;
