@@ -8,7 +8,7 @@
 // the largest of 32 goes over 4 (or 8) lanes.  Parameter gradients are summed in a fixed order: dw in each lane, then over the lanes,
 // waves and workgroups one after the other; dd as a value per row, then over slabs of tokens.
 // Bound by HBM, 4 x 4 096 tokens of 16 heads of 128 in 16 bits: front end with checkpoints 98 us (5.1 TB/s), from them 69 (4.4), its backward 106
-// (4.8); back end with checkpoints 56 (4.8), its backward 64 (4.2).
+// (4.8); back end with checkpoints 56 (4.8), its backward 64 (4.2); one tensor's checkpoint by itself 18, read back 16 (out of the last-level cache in part).
 #include "mdn_kept_rules.h"
 #include "mdn_layer_rows.h"
 
