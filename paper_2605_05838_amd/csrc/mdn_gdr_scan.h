@@ -222,20 +222,9 @@ template <typename T, int T0 = 0, int NT> __device__ __forceinline__ void save_s
         for (int x = 0; x < 4; ++x) g[(size_t)(Gd<T>::row(T0 + t, 4 * kg) + x) * dv + col + r] = S[t][x];
 }
 
-// Whether a scan brings later chunks' operands into the L2 (GdrTouch).  In 16 bits only where the rows and states of the call are more than one
-// and a quarter times what the last-level cache holds, whose latency the loads cover.  In us, without / with, 16 heads of 128: forward and
-// backward keeping states, by the forward scan, 8 192 tokens 433 / 425, 12 288 623 / 620, 16 384 847 / 821, 24 576 1 311 / 1 212, 32 768 1 721 / 1 596;
-// nothing but the forward 8 192 142 / 143, 16 384 268 / 327, 20 480 423 / 410, 24 576 571 / 500, 32 768 766 / 664.  In fp32 always: 8 192 tokens
-// 556 / 554 (with kept states 560 / 540).  With remainders never: the chain is what a step waits for (32 768 tokens 857 / 895).
-// With 32 columns, where every CU is at work, the forward does for the kept states' sake and only where the states have 128 columns: forward and backward,
-// 8 x 4 096 942 / 920, 4 x 8 192 929 / 900, dk = 64 687 / 681, but dv = 64 633 / 641, heads of 64 with 8 x 8 192 983 / 999; without kept states 4 x 8 192
-// 279 / 288, heads of 64 with 8 x 8 192 330 / 356 (forward).
-// The reverse scan always does, but with remainders; backward call: 8 192 tokens 256 / 235, 32 768 1 071 / 926, 8 x 2 048 of 8 heads 144 / 139,
-// 4 x 4 096 309 / 274, 777 33.7 / 33.6, 8 192 in fp32 1 019 / 919, [2, 1 024] of 4 heads of 64 67.3 / 67.8.
-inline bool gdr_touch_pays(const GdrDims &d, int key_rows, int value_rows, bool states) {
-    if (d.dtype == 1) return true;
-    const size_t block = 64 * (size_t)(key_rows * d.dk + value_rows * d.dv) * 2 + (states ? (size_t)d.dk * d.dv * 2 : 0);
-    return (size_t)d.nchunks * d.H * block > 5 * kLastLevelCache / 4;
+// see gdr_bytes
+inline size_t gdr_call_bytes(const GdrDims &d, int key_rows, int value_rows, bool states) {
+    return gdr_bytes((size_t)d.nchunks * d.H, d.dk, d.dv, key_rows, value_rows, states);
 }
 
 // which of its two forms a scan takes: see sixteen_columns

@@ -400,7 +400,7 @@ template <typename T, int DK, bool PRECISE, bool REBUILD> hipError_t launch(cons
 
 hipError_t launch_gdr_scan_fwd(const GdrDims &d, const GdrScanFwdArgs &args, bool precise, hipStream_t s) {
     GdrScanFwdArgs a = args;
-    a.touch = !precise && gdr_touch_pays(d, 2, args.e ? 3 : 2, args.states) && (d.dtype == 1 || gdr_one_group(d) || (args.states && d.dv == 128));
+    a.touch = !precise && gdr_forward_touch(d.dtype == 1, gdr_one_group(d), d.dv, args.states, gdr_call_bytes(d, 2, args.e ? 3 : 2, args.states));
     if (d.dtype == 1) return d.dk == 64 ? launch<float, 64, false, false>(d, a, s) : launch<float, 128, false, false>(d, a, s);
     if (precise) return d.dk == 64 ? launch<bf16_t, 64, true, false>(d, a, s) : launch<bf16_t, 128, true, false>(d, a, s);
     return d.dk == 64 ? launch<bf16_t, 64, false, false>(d, a, s) : launch<bf16_t, 128, false, false>(d, a, s);
@@ -408,7 +408,7 @@ hipError_t launch_gdr_scan_fwd(const GdrDims &d, const GdrScanFwdArgs &args, boo
 
 hipError_t launch_gdr_rebuild(const GdrDims &d, const GdrScanFwdArgs &args, hipStream_t s) {
     GdrScanFwdArgs a = args;
-    a.touch = gdr_touch_pays(d, 1, 1, true);
+    a.touch = d.dtype == 1 || gdr_touch_pays(gdr_call_bytes(d, 1, 1, true));
     if (d.dtype == 1) return d.dk == 64 ? launch<float, 64, false, true>(d, a, s) : launch<float, 128, false, true>(d, a, s);
     return d.dk == 64 ? launch<bf16_t, 64, false, true>(d, a, s) : launch<bf16_t, 128, false, true>(d, a, s);
 }

@@ -44,6 +44,26 @@ constexpr bool q_tile_pays(int columns, int d, size_t pairs, size_t chunks, size
     return d == 64 ? vt || pairs >= 4 : bytes > (vt ? 4 : 5) * kLastLevelCache / 4;
 }
 
+// Bytes of the 16-bit rows and states of a scan of the gated delta rule over `blocks` chunk blocks
+constexpr size_t gdr_bytes(size_t blocks, int dk, int dv, int key_rows, int value_rows, bool states) {
+    return blocks * (64 * (size_t)(key_rows * dk + value_rows * dv) * 2 + (states ? (size_t)dk * dv * 2 : 0));
+}
+
+// Gated delta rule: whether a scan brings later chunks' operands into the L2 (GdrTouch).  In 16 bits only where the rows and states of the call are more than one
+// and a quarter times what the last-level cache holds, whose latency the loads cover.  In us, without / with, 16 heads of 128: forward and
+// backward keeping states, by the forward scan, 8 192 tokens 433 / 425, 12 288 623 / 620, 16 384 847 / 821, 24 576 1 311 / 1 212, 32 768 1 721 / 1 596;
+// nothing but the forward 8 192 142 / 143, 16 384 268 / 327, 20 480 423 / 410, 24 576 571 / 500, 32 768 766 / 664.  In fp32 always: 8 192 tokens
+// 556 / 554 (with kept states 560 / 540).  With remainders never: the chain is what a step waits for (32 768 tokens 857 / 895).
+// With 32 columns, where every CU is at work, the forward does for the kept states' sake and only where the states have 128 columns: forward and backward,
+// 8 x 4 096 942 / 920, 4 x 8 192 929 / 900, dk = 64 687 / 681, but dv = 64 633 / 641, heads of 64 with 8 x 8 192 983 / 999; without kept states 4 x 8 192
+// 279 / 288, heads of 64 with 8 x 8 192 330 / 356 (forward).
+// The reverse scan always does, but with remainders; backward call: 8 192 tokens 256 / 235, 32 768 1 071 / 926, 8 x 2 048 of 8 heads 144 / 139,
+// 4 x 4 096 309 / 274, 777 33.7 / 33.6, 8 192 in fp32 1 019 / 919, [2, 1 024] of 4 heads of 64 67.3 / 67.8.
+constexpr bool gdr_touch_pays(size_t bytes) { return bytes > 5 * kLastLevelCache / 4; }
+constexpr bool gdr_forward_touch(bool f32, bool sixteen, int dv, bool states, size_t bytes) {
+    return f32 || (gdr_touch_pays(bytes) && (sixteen || (states && dv == 128)));
+}
+
 // Gated delta rule: 16 columns per workgroup while there is a CU for each of these workgroups, or 32.  `sequences` of `chunks` chunks together
 // (0: of equal lengths), the longest of `longest`.  Calls in us, 16 / 32 columns, heads of 128: forward with kept states, with final states,
 // backward, with adjoints of the initial states: 777 tokens of 16 heads 22.8 / 23.8, 28.0 / 32.7, 33.6 / 35.9, 49 / 54;
