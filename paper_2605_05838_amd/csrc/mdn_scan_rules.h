@@ -69,12 +69,15 @@ constexpr bool gdr_forward_touch(bool f32, bool sixteen, int dv, bool states, si
 // backward, with adjoints of the initial states: 777 tokens of 16 heads 22.8 / 23.8, 28.0 / 32.7, 33.6 / 35.9, 49 / 54;
 // 2 x 2 048 (256 workgroups of 16 columns) 50 / 52, 62 / 73, 84 / 89, 119 / 128; 3 x 2 048 (384) 90 / 60, 115 / 81, 143 / 108, 205 / 157;
 // 8 x 2 048 246 / 147, 238 / 160, 341 / 278, 479 / 385; heads of 64, where two would share a CU, 8 x 2 048 (512) 100 / 77, 109 / 79, 149 / 135, 223 / 184.
-// Packed sequences count by the longest one: what is to be done beside its chain is the others' chunks, not their number.  16 heads of 128,
-// 16 384 and 20 x 64 tokens 382 / 382, 434 / 485, 541 / 579, 711 / 787; 4 096 and 20 x 64 91 / 91, 116 / 135, 159 / 169, 199 / 217; 4 096 and
-// 20 x 512 216 / 127, 236 / 162, 362 / 308, 445 / 356; 4 096, 2 048, 1 024 and 10 x 300 128 / 105, 166 / 147, 260 / 242, 317 / 291; 2 x 8 192 and
-// 40 x 32 323 / 255, 344 / 289, 484 / 429, 605 / 557; 3 x 777 43 / 30, 56 / 40, 84 / 69, 100 / 80.
+// Packed sequences count by the longest one: what is to be done beside its chain is the others' steps, of which a sequence has two more than
+// chunks, not their number.  16 heads of 128, 16 384 and 20 x 64 tokens 382 / 382, 434 / 485, 541 / 579, 711 / 787, and 100 x 64 463 / 482, 529 / 529,
+// 646 / 644, 811 / 886, and 60 x 1 388 / 392, 456 / 490, 556 / 596, 740 / 814, and 150 x 1 476 / 441, 579 / 530, 716 / 648, 889 / 891; 32 768 and
+// 500 x 1 1 324 / 1 033, 1 584 / 1 141, 1 884 / 1 400, 2 354 / 1 989; 4 096 and 20 x 64 91 / 91, 116 / 135, 159 / 169, 199 / 217, and 40 x 1 116 / 93,
+// 145 / 137, 195 / 179, 234 / 226, and 20 x 512 216 / 127, 236 / 162, 362 / 308, 445 / 356; 8 192 and 4 x 1 000 202 / 188, 223 / 258, 324 / 344,
+// 408 / 441; 2 048, 1 500 and 8 x 20 60 / 54, 77 / 75, 110 / 105, 131 / 130; 2 x 8 192 and 40 x 32 323 / 255, 344 / 289, 484 / 429, 605 / 557;
+// 3 x 777 43 / 30, 56 / 40, 84 / 69, 100 / 80.
 constexpr bool sixteen_columns(size_t sequences, size_t chunks, size_t longest, size_t heads, int dv, size_t cus) {
-    const size_t beside = chunks ? (chunks + longest - 1) / longest : sequences;
+    const size_t beside = chunks ? (chunks + 2 * sequences + longest + 1) / (longest + 2) : sequences;
     return (beside * heads + 7) / 8 * 8 * (size_t)(dv / 16) <= cus;
 }
 

@@ -44,7 +44,9 @@ def test_equal_lengths(sixteen, B, T, H, dv, columns):
 
 @pytest.mark.parametrize("lens,columns", [([16384] + [64] * 20, 16), ([4096] + [64] * 20, 16), ([4096] + [512] * 20, 32),
                                           ([4096, 2048, 1024] + [300] * 10, 32), ([8192] * 2 + [32] * 40, 32), ([777] * 3, 32), ([777], 16),
-                                          ([1] * 300, 32)])
+                                          ([1] * 300, 32), ([16384] + [1] * 60, 16), ([16384] + [1] * 150, 32), ([32768] + [1] * 500, 32),
+                                          ([4096] + [1] * 20, 16), ([4096] + [1] * 40, 32), ([8192] + [1000] * 4, 16),
+                                          ([2048, 1500] + [20] * 8, 32), ([2048] + [64] * 10, 16)])
 def test_packed_where_it_was_faster(sixteen, lens, columns):
     """16 heads of 128: sequences beside one long one count by what there is to do beside it."""
     chunks = [(n + 63) // 64 for n in lens]
@@ -61,3 +63,10 @@ def test_lines_into_the_l2(rules, B, T, H, dk, dv, kept, faster):
     chunks = (T + 63) // 64
     assert rules.touch(False, rules.sixteen(B, 0, chunks, H, dv), B * H * chunks, dk, dv, kept) is faster
     assert rules.touch(True, rules.sixteen(B, 0, chunks, H, dv), B * H * chunks, dk, dv, kept) # fp32: always
+
+
+def test_packed_sequences_of_equal_lengths_are_a_batch(sixteen):
+    for B in (1, 2, 3, 5, 40):
+        for n in (1, 2, 13, 512):
+            for H in (1, 7, 16, 100):
+                assert sixteen(B, B * n, n, H, 128) == sixteen(B, 0, n, H, 128)
